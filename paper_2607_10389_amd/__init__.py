@@ -7,6 +7,11 @@ decode fused with re-checksumming and an all-or-nothing install on the
 destination.  The work runs in the HIP kernels of ``libwm.so``; this package
 is its Python binding (``_wm``) plus a small buffer-owning helper
 (``mover.Mover``).
+
+Next to the mover stands the cache that a moved session answers from: 8-bit
+codes in blocks of tokens, with block tables and slot maps, the store of new
+keys and values, attention, and a session's blocks to and from the flat state
+(``_cache``; ``paged.PagedCache`` owns the buffers).
 """
 from . import _wm
 from ._wm import (  # noqa: F401
@@ -16,5 +21,10 @@ from ._wm import (  # noqa: F401
     decode_verify, diff_dirty, encode, encode_step, flat_bytes, flatten,
     manifest_ws_bytes, params, payload_bound, rehydrate, workspace_bytes,
 )
+from ._cache import (  # noqa: F401
+    PoolTable, attend_ws_bytes, cache_append, cache_attend, flat_pages_bytes, flatten_pages,
+    page_tables, rehydrate_pages,
+)
 from .mover import Mover  # noqa: F401
+from .paged import PagedCache  # noqa: F401
 from . import precopy  # noqa: F401

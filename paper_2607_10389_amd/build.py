@@ -20,7 +20,9 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build", "wm")
 LIB = os.path.join(HERE, "libwm.so")
 
-SOURCES = ["wm_kernels.hip", "wm_tables.cpp", "wm_api.cpp"]
+SOURCES = ["wm_kernels.hip", "wm_tables.cpp", "wm_api.cpp",
+           "wm_cache_kernels.hip", "wm_cache_api.cpp", "wm_attend_64.hip",
+           "wm_attend_128.hip", "wm_attend_192.hip", "wm_attend_256.hip"]
 ARCH = "gfx950"
 
 

@@ -1,0 +1,126 @@
+"""A paged 8-bit attention cache that owns its buffers, and its sessions' way
+to and from the mover.
+
+A ``PagedCache`` holds one pool of blocks for every layer, the block tables
+and lengths of its requests, and the ring of free blocks.  ``step`` gives
+requests room for their new tokens (or takes it back), ``append`` and
+``attend`` are one layer's store and attention for those tokens, and
+``suspend`` / ``resume`` are a session's way out and in: a flat state of every
+layer's blocks, which a ``Mover`` ships like any other, into whichever blocks
+the destination has free.  The session's answers after a move are the same
+bits as before it: they do not depend on where its blocks lie.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _cache, _wm
+
+
+class PagedCache:
+    def __init__(self, layers: int, blocks: int, heads: int, dim: int, block_tokens: int = 64,
+                 dtype: torch.dtype = torch.float8_e4m3fn, max_requests: int = 64,
+                 max_blocks: int | None = None, device: str | torch.device = "cuda"):
+        self.layers, self.heads, self.dim, self.block_tokens = layers, heads, dim, block_tokens
+        self.max_requests = max_requests
+        i32 = dict(dtype=torch.int32, device=torch.device(device))
+        # a block of all layers is one piece: a session moves in large copies
+        self.codes = torch.zeros(blocks, layers, 2, heads * block_tokens * dim,
+                                 dtype=torch.uint8, device=i32["device"])
+        self.scales = torch.zeros(blocks, layers, 2, heads, dtype=torch.float32,
+                                  device=i32["device"])
+        self._layers = []
+        for n in range(layers):
+            k, v = (self.codes[:, n, i].view(dtype) for i in (0, 1))
+            self._layers.append((k.view(blocks, heads, block_tokens, dim),
+                                 v.view(blocks, heads, dim, block_tokens),
+                                 self.scales[:, n, 0], self.scales[:, n, 1]))
+        self.block_table = torch.zeros(max_requests, max_blocks or blocks, **i32)
+        self.ring = torch.arange(blocks, **i32)
+        self.pool = torch.tensor([0, blocks], **i32)
+        self._pool_next = torch.zeros(2, **i32)
+        self.lens = torch.zeros(max_requests, **i32)
+        self.lengths = [0] * max_requests  # the same on the host
+        self.q_start = torch.zeros(max_requests + 1, **i32)
+        self.slot_map = torch.zeros(0, dtype=torch.int64, device=i32["device"])
+        self.verdict = torch.zeros(1, **i32)
+        self._ws = torch.zeros(0, dtype=torch.uint8, device=i32["device"])
+        self.pools = _cache.PoolTable([self.codes, self.scales])
+
+    def layer(self, n: int):
+        """(key codes, value codes, key scales, value scales) of layer n."""
+        return self._layers[n]
+
+    def step(self, new_lengths: dict[int, int]) -> int:
+        """Take requests to new lengths (0: done); the others stay.  Returns
+        the number of new tokens, whose keys, values and queries append() and
+        attend() expect ordered by request.  Waits for the verdict; raises
+        WmError, and changes nothing, if the pool or the tables are too small."""
+        want = list(self.lengths)
+        for r, n in new_lengths.items():
+            want[r] = n
+        tokens = sum(max(0, n - o) for o, n in zip(self.lengths, want))
+        new = torch.tensor(want, dtype=torch.int32).to(self.lens.device)
+        slots = self.slot_map
+        if slots.numel() < tokens:
+            slots = torch.zeros(tokens, dtype=torch.int64, device=self.lens.device)
+        _cache.page_tables(self.lens, new, self.block_tokens, self.block_table, self.ring,
+                           self.pool, self._pool_next, slots, self.q_start, self.verdict)
+        bits = int(self.verdict.item())
+        if bits:
+            raise _wm.WmError(_wm.WM_ERR_CAPACITY, f"step (verdict {bits})")
+        self.pool, self._pool_next = self._pool_next, self.pool
+        self.lens, self.lengths, self.slot_map = new, want, slots
+        return tokens
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Store the step's new keys and values [tokens, heads, dim]."""
+        _cache.cache_append(k, v, *self._layers[layer], self.slot_map, self.q_start,
+                            self.verdict)
+
+    def attend(self, layer: int, q: torch.Tensor, scale: float, window: int = 0,
+               out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
+        """Attention of the step's new tokens [tokens, query heads, dim]."""
+        c = self._layers[layer]
+        most = max(self.lengths)
+        need = _cache.attend_ws_bytes(q, c[0], self.lens, most)
+        if self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        out = torch.empty_like(q) if out is None else out
+        _cache.cache_attend(q, *c, self.block_table, self.lens, self.q_start, out, self._ws,
+                            max_len=most, scale=scale, window=window, lse=lse,
+                            verdict=self.verdict)
+        return out
+
+    # ---- a session's move
+    def _blocks(self, length: int) -> int:
+        return -(-length // self.block_tokens)
+
+    def flat_bytes(self, length: int) -> int:
+        """Bytes of the flat state of a session of this length."""
+        return _cache.flat_pages_bytes(self.pools, self._blocks(length))
+
+    def suspend(self, request: int, flat: torch.Tensor | None = None) -> torch.Tensor:
+        """The request's blocks of every layer as one flat state; the request
+        stays (step({request: 0}) frees its blocks)."""
+        n = self._blocks(self.lengths[request])
+        if flat is None:
+            flat = torch.empty(self.flat_bytes(self.lengths[request]), dtype=torch.uint8,
+                               device=self.codes.device)
+        self.verdict.zero_()
+        _cache.flatten_pages(self.pools, self.block_table[request, :n], flat, self.verdict)
+        return flat
+
+    def resume(self, request: int, length: int, flat: torch.Tensor,
+               verdict: torch.Tensor | None = None) -> None:
+        """Give an empty request blocks for a session of this length and
+        install its flat state there, if the verdict word (wm_decode_verify's,
+        say) is 0 on the device.  The next call is a step()."""
+        if self.lengths[request]:
+            raise ValueError(f"request {request} holds a session")
+        self.step({request: length})
+        n = self._blocks(length)
+        if verdict is None:
+            self.verdict.zero_()
+            verdict = self.verdict
+        _cache.rehydrate_pages(flat, self.pools, self.block_table[request, :n], verdict)

@@ -1,0 +1,650 @@
+"""GPU parity of the paged 8-bit cache (include/wm_cache.h) against plain
+whole-number and 64-bit references: block tables and slot maps, stored codes
+and scales, attention, blocks to and from the flat state, and a session moved
+with all of them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as ref
+from gpu_helpers import random_bytes, say
+
+pytestmark = pytest.mark.gpu
+
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+BF, HF = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def wm():
+    from paper_2607_10389_amd import _cache
+    return _cache
+
+
+def dev(x, dtype=torch.int32):
+    return torch.as_tensor(x, dtype=dtype).cuda()
+
+
+def word():
+    return dev([0])
+
+
+# ---- block tables and slot maps ----------------------------------------------
+
+
+def run_tables(wm, old, new, bt, width, ring, head, count, slot_cap, seed=0, stride=None):
+    g = np.random.default_rng(seed)
+    n = len(old)
+    stride = stride or width
+    table = g.integers(0, 1 << 20, (n, stride)).tolist()
+    slots = (-g.integers(1, 1000, slot_cap)).tolist()
+    q0 = [-7] * (n + 1)
+    want = ref.tables(old, new, bt, [r[:width] for r in table], ring, head, count, slots, q0)
+    t = dev(table).reshape(n, stride)
+    rg, pi, po = dev(ring), dev([head, count]), dev([-1, -1])
+    sl, qs, v = dev(slots, torch.int64), dev(q0), dev([77])
+    for _ in range(2):  # the same again: same inputs, same outputs
+        wm.page_tables(dev(old), dev(new), bt, t[:, :width], rg, pi, po, sl, qs, v)
+        torch.cuda.synchronize()
+        assert int(v.item()) == want[5]
+        got = t.cpu().tolist()
+        assert [r[:width] for r in got] == want[0]
+        assert [r[width:] for r in got] == [r[width:] for r in table]
+        assert rg.cpu().tolist() == want[1]
+        assert po.cpu().tolist() == want[2]
+        assert sl.cpu().tolist() == want[3]
+        assert qs.cpu().tolist() == want[4]
+        assert pi.cpu().tolist() == [head, count]
+    return want
+
+
+@pytest.mark.parametrize("n,bt,most,seed", [(1, 16, 40, 0), (5, 64, 300, 1), (64, 32, 500, 2),
+                                            (1024, 16, 90, 3), (1025, 128, 700, 4),
+                                            (2500, 16, 40, 5)])
+def test_tables_of_random_steps(wm, n, bt, most, seed):
+    say(f"[tables] n={n} bt={bt} most={most}")
+    g = np.random.default_rng(seed)
+    old = g.integers(0, most + 1, n)
+    new = np.where(g.random(n) < 0.3, g.integers(0, most + 1, n), old + 1)
+    new = np.where(g.random(n) < 0.2, 0, new)
+    width = -(-(most + 1) // bt)
+    up = lambda x: -(-x // bt)  # noqa: E731
+    need = int(np.maximum(0, up(new) - up(old)).sum())
+    give = int(np.maximum(0, up(old) - up(new)).sum())
+    count = need + 3
+    cap = count + give + 5
+    ring = g.permutation(cap * 2)[:cap].tolist()
+    tokens = int(np.maximum(0, new - old).sum())
+    run_tables(wm, old.tolist(), new.tolist(), bt, width, ring, cap - 2, count, tokens + 9, seed,
+               stride=width + 3)
+
+
+def test_tables_of_no_requests_and_of_no_change(wm):
+    run_tables(wm, [5, 0, 64], [5, 0, 64], 64, 4, [1, 2, 3], 0, 3, 4)
+    v, po, qs = dev([9]), dev([5, 5]), dev([3])
+    e = dev([])
+    wm.page_tables(e, e, 64, torch.zeros(0, 4, dtype=torch.int32, device="cuda"), dev([1, 2]),
+                   dev([1, 2]), po, dev([], torch.int64), qs, v)
+    assert v.item() == 0 and po.tolist() == [1, 2] and qs.tolist() == [0]
+
+
+def test_tables_of_one_long_request(wm):
+    # every workgroup writes slots of the same request
+    run_tables(wm, [37, 3], [150_000, 4], 16, 9400, list(range(10_000)), 9_990, 9_800, 150_000)
+
+
+@pytest.mark.parametrize("old,new,count,slots,verdict", [
+    ([0, 10], [-1, 11], 9, 40, 1), ([0, -5], [3, 11], 9, 40, 1), ([0, 1], [3, 65], 9, 99, 1),
+    ([65, 1], [0, 2], 9, 99, 1), ([0, 16], [33, 17], 3, 40, 2), ([0, 16], [33, 17], 4, 33, 4),
+    ([0, 16], [33, 17], 4, 34, 0), ([64, 16], [0, 17], 9, 40, 2), ([0, 16], [33, 17], 3, 3, 6)])
+def test_tables_that_are_refused_change_nothing(wm, old, new, count, slots, verdict):
+    want = run_tables(wm, old, new, 16, 4, list(range(100, 112)), 7, count, slots)
+    assert want[5] == verdict
+
+
+# ---- stored codes ----------------------------------------------------------------
+
+
+def make_cache(blocks, heads, bt, dim, fmt, seed, stride=0, spread=True):
+    """Codes and scales in a pool whose blocks lie `stride` bytes further
+    apart than they need to."""
+    g = torch.Generator().manual_seed(seed)
+    page = heads * bt * dim
+    out = []
+    for shape in ((heads, bt, dim), (heads, dim, bt)):
+        x = (torch.randn(blocks, page, generator=g) * ref.LARGEST[fmt] / 8).to(fmt)
+        pool = torch.zeros(blocks, page + stride, dtype=torch.uint8)
+        pool[:, :page] = x.view(torch.uint8)
+        out.append(pool.cuda()[:, :page].view(fmt).view(blocks, *shape))
+    for _ in range(2):
+        e = torch.randint(-9, -5, (blocks, heads), generator=g).float()
+        s = torch.exp2(e)
+        if spread:
+            s = s * (1 + torch.rand(blocks, heads, generator=g))
+        pool = torch.zeros(blocks, heads + stride // 16)
+        pool[:, :heads] = s
+        out.append(pool.cuda()[:, :heads])
+    return out
+
+
+def layout(lens, bt, seed, extra=3):
+    """Block table rows of a shuffled pool for these lengths: (rows, blocks)."""
+    g = np.random.default_rng(seed)
+    need = [-(-n // bt) for n in lens]
+    blocks = sum(need) + extra
+    ids = g.permutation(blocks).tolist()
+    width = max(need + [1])
+    rows, at = [], 0
+    for c in need:
+        rows.append(ids[at:at + c] + [-5] * (width - c))
+        at += c
+    return rows, blocks
+
+
+APPENDS = [
+    # old lengths, new tokens, heads, bt, dim, type, format, block stride
+    ([0], [1], 1, 16, 64, BF, E4, 0),
+    ([5, 0, 31, 64], [1, 1, 1, 1], 2, 32, 128, BF, E4, 64),
+    ([0, 17, 3], [130, 40, 0], 3, 64, 64, HF, E5, 0),
+    ([1, 255, 0], [300, 2, 256], 2, 256, 192, BF, E5, 32),
+    ([15, 16, 33], [1, 50, 16], 1, 16, 256, HF, E4, 0),
+    ([0, 100], [129, 29], 2, 128, 128, HF, E4, 16),
+]
+
+
+@pytest.mark.parametrize("old,new,heads,bt,dim,dt,fmt,stride", APPENDS)
+def test_stored_codes_and_scales(wm, old, new, heads, bt, dim, dt, fmt, stride):
+    say(f"[append] old={old} new={new} heads={heads} bt={bt} dim={dim} {dt} {fmt}")
+    rows, blocks = layout([o + n for o, n in zip(old, new)], bt, 1)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, fmt, 2, stride)
+    starts = [0] + np.cumsum(new).tolist()
+    slots = [rows[r][(o + i) // bt] * bt + (o + i) % bt
+             for r, (o, n) in enumerate(zip(old, new)) for i in range(n)]
+    g = torch.Generator().manual_seed(3)
+    total = starts[-1]
+    # a packed projection's rows, with magnitudes from far below the scales
+    # to far above them, by token
+    qkv = torch.randn(total + 2, 3 * heads + 1, dim, generator=g)
+    qkv *= torch.exp2(torch.randint(-12, 7, (total + 2, 1, 1), generator=g).float())
+    qkv[::5] = 0.0
+    qkv = qkv.to(dt).cuda()
+    kn, vn = qkv[:, heads:2 * heads], qkv[:, 2 * heads:3 * heads]
+    want_k, want_ks = ref.append(kn.cpu(), k.cpu(), ks.cpu(), slots, starts, False)
+    want_v, want_vs = ref.append(vn.cpu(), v.cpu(), vs.cpu(), slots, starts, True)
+    verdict = word()
+    for _ in range(2):  # storing the same again changes nothing
+        wm.cache_append(kn, vn, k, v, ks, vs, dev(slots + [-1, -1], torch.int64), dev(starts),
+                        verdict)
+        torch.cuda.synchronize()
+        assert verdict.item() == 0
+        assert torch.equal(ks.cpu().double(), want_ks) and torch.equal(vs.cpu().double(), want_vs)
+        assert torch.equal(ref.decode(k.cpu()), want_k)
+        assert torch.equal(ref.decode(v.cpu()), want_v)
+
+
+def test_stored_infinities_nan_and_extremes(wm):
+    heads, bt, dim = 1, 16, 64
+    for fmt in (E4, E5):
+        k, v, ks, vs = make_cache(4, heads, bt, dim, fmt, 5)
+        x = torch.zeros(6, heads, dim)
+        x[0, 0, :4] = torch.tensor([math.inf, -math.inf, math.nan, 3.0])
+        x[1] = 3.38e38        # the largest magnitudes of the type
+        x[2] = 1e-38
+        x[3] = -0.0
+        x[4, 0, 0] = math.nan  # nothing finite but zeros
+        x[5] = 448.0
+        xb = x.to(BF).cuda()
+        # tokens 0..3 fresh blocks of their own, 4 and 5 into a block in use
+        slots, starts = [0, 16, 32, 48, 49, 50], [0, 1, 2, 3, 6]
+        want_k, want_ks = ref.append(xb.cpu(), k.cpu(), ks.cpu(), slots, starts, False)
+        want_v, want_vs = ref.append(xb.cpu(), v.cpu(), vs.cpu(), slots, starts, True)
+        wm.cache_append(xb, xb, k, v, ks, vs, dev(slots, torch.int64), dev(starts))
+        torch.cuda.synchronize()
+        assert torch.equal(ks.cpu().double(), want_ks) and torch.equal(vs.cpu().double(), want_vs)
+        for got, want in ((k, want_k), (v, want_v)):
+            got = ref.decode(got.cpu())
+            assert torch.equal(got.isnan(), want.isnan())
+            assert torch.equal(got.nan_to_num(), want.nan_to_num())
+        assert bool(torch.isfinite(ks).all())
+
+
+def test_every_code_survives_the_store(wm):
+    """Each finite code's value, stored, comes back as that code."""
+    for fmt in (E4, E5):
+        codes = torch.arange(256, dtype=torch.int32).to(torch.uint8).view(fmt).float()
+        codes = torch.where(torch.isfinite(codes), codes, torch.zeros_like(codes))
+        x = torch.zeros(4, 1, 64)
+        x.view(-1)[:] = codes
+        # each row has the largest magnitude once, so the scale is 1
+        x[:, 0, 0] = ref.LARGEST[fmt]
+        k, v, ks, vs = make_cache(1, 1, 16, 64, fmt, 6)
+        xb = x.to(BF).cuda()
+        wm.cache_append(xb, xb, k, v, ks, vs, dev([0, 1, 2, 3], torch.int64), dev([0, 4]))
+        assert ks.item() == 1.0 and vs.item() == 1.0
+        assert torch.equal(k[0, 0, :4].float().cpu(), x[:, 0])
+        assert torch.equal(v[0, 0, :, :4].float().cpu(), x[:, 0].t())
+        assert not k[0, 0, 4:].float().any() and not v[0, 0, :, 4:].float().any()
+
+
+def test_slots_outside_and_starts_beyond(wm):
+    k, v, ks, vs = make_cache(3, 2, 16, 64, E4, 7)
+    before = [t.clone() for t in (k.view(torch.uint8), v.view(torch.uint8), ks, vs)]
+    x = torch.randn(4, 2, 64).to(BF).cuda()
+    verdict = word()
+
+    def same():
+        torch.cuda.synchronize()
+        now = (k.view(torch.uint8), v.view(torch.uint8), ks, vs)
+        return all(torch.equal(a, b) for a, b in zip(now, before))
+    # padding rows
+    wm.cache_append(x, x, k, v, ks, vs, dev([-1] * 4, torch.int64), dev([0, 2, 4]), verdict)
+    assert same() and verdict.item() == 0
+    # beyond the pool
+    wm.cache_append(x, x, k, v, ks, vs, dev([48, 1 << 40, 1 << 33, 99], torch.int64),
+                    dev([0, 1, 2, 3, 4]), verdict)
+    assert same() and verdict.item() == 8
+    # starts beyond the rows: the rows that are there are stored
+    verdict = word()
+    want_k, _ = ref.append(x.cpu(), k.cpu(), ks.cpu(), [5, 6, 7, 8], [0, 4], False)
+    wm.cache_append(x, x, k, v, ks, vs, dev([5, 6, 7, 8], torch.int64), dev([0, 30]), verdict)
+    torch.cuda.synchronize()
+    assert verdict.item() == 4
+    assert torch.equal(ref.decode(k.cpu()), want_k)
+
+
+# ---- attention ---------------------------------------------------------------------
+
+
+def values(codes, scale, transposed):
+    x = ref.decode(codes.cpu())
+    x = x.transpose(2, 3) if transposed else x
+    return (x * scale.cpu().double()[:, :, None, None]).contiguous()
+
+
+def check_attend(wm, lens, new, heads, group, bt, dim, dt, fmt, window=0, seed=0, stride=0,
+                 pad=2, max_len=None, packed=True, tail=None, scale=None, spread=1.5):
+    say(f"[attend] lens={lens} new={new} heads={heads}x{group} bt={bt} dim={dim} {dt} {fmt} "
+        f"window={window}")
+    rows, blocks = layout(lens, bt, seed)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, fmt, seed + 1, stride)
+    starts = [0] + np.cumsum(new).tolist()
+    total, hq = starts[-1], heads * group
+    g = torch.Generator().manual_seed(seed + 2)
+    scale = scale if scale is not None else 1 / math.sqrt(dim)
+    wide = torch.randn(total + pad, hq + (3 if packed else 0), dim, generator=g) * spread
+    q = wide.to(dt).cuda()[:, :hq]
+    if tail is not None:
+        tail(k, v, ks, vs, rows)
+    out = torch.full((total + pad, hq, dim + 8), 7.0, dtype=dt, device="cuda")[..., :dim]
+    lse = torch.full((total + pad, hq), 7.0, device="cuda")
+    verdict = word()
+    table, most = dev(rows), max_len if max_len is not None else max(lens)
+    n = wm.attend_ws_bytes(q, k, dev(lens), most)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    wm.cache_attend(q, k, v, ks, vs, table, dev(lens), dev(starts), out, ws, max_len=most,
+                    scale=scale, window=window, lse=lse, verdict=verdict)
+    torch.cuda.synchronize()
+    assert verdict.item() == 0
+    want, z, weight, sp = ref.attend(q.cpu(), values(k, ks, False), values(v, vs, True), rows,
+                                     lens, starts, bt, scale, window)
+    bo, bl = ref.attend_bound(dt, want, z, weight, sp, max(lens + [1]), dim)
+    got, got_z = out[:total].cpu().double(), lse[:total].cpu().double()
+    assert bool((out[total:].cpu() == 7.0).all()) and bool((lse[total:].cpu() == 7.0).all())
+    empty = torch.isinf(z[:total])
+    assert torch.equal(empty, torch.isneginf(got_z))
+    assert not got[empty].any()
+    off = (got - want[:total]).abs()
+    assert bool((off <= bo[:total]).all()), float((off / bo[:total]).max())
+    zoff = torch.where(empty, torch.zeros_like(z[:total]), (got_z - z[:total]).abs())
+    assert bool((zoff <= bl[:total]).all()), float((zoff / bl[:total]).max())
+    # the same bits again
+    again = torch.full_like(out, 7.0)
+    wm.cache_attend(q, k, v, ks, vs, table, dev(lens), dev(starts), again, ws, max_len=most,
+                    scale=scale, window=window)
+    assert torch.equal(again, out)
+
+
+ATTENDS = [
+    # lengths, new tokens, heads, group, bt, dim, type, format, more
+    ([1], [1], 1, 1, 16, 64, BF, E4, {}),
+    ([1, 2, 15, 16, 17, 63, 64, 65, 127], [1] * 9, 2, 4, 16, 64, BF, E4, {}),
+    ([512], [1], 8, 1, 64, 64, BF, E4, {}),
+    ([130, 64, 200], [1, 1, 1], 2, 8, 64, 128, HF, E5, {}),
+    ([33, 300], [1, 1], 1, 16, 32, 192, BF, E5, {}),
+    ([77, 513], [1, 1], 2, 3, 128, 256, HF, E4, dict(stride=48)),
+    ([260, 5], [1, 2], 1, 32, 256, 128, BF, E4, dict(stride=16)),
+    # prompts and chunks: rows that see different lengths
+    ([5, 37, 64], [5, 20, 1], 2, 4, 16, 64, BF, E4, {}),
+    ([100, 201], [100, 65], 1, 2, 64, 128, BF, E4, {}),
+    ([90, 33], [70, 33], 2, 1, 32, 128, HF, E5, {}),
+    ([64, 130], [33, 64], 1, 5, 16, 256, HF, E4, {}),
+    ([150], [150], 1, 7, 128, 192, BF, E5, {}),
+    # windows: shorter than a step, across blocks, longer than the sequence
+    ([200, 90, 65], [1, 1, 1], 2, 2, 16, 64, BF, E4, dict(window=1)),
+    ([200, 90, 300], [40, 90, 1], 1, 4, 32, 128, BF, E4, dict(window=37)),
+    ([100, 40], [30, 40], 1, 2, 64, 64, HF, E5, dict(window=1000)),
+    # requests without tokens, without queries, and queries before the start
+    ([0, 50, 0, 7], [1, 0, 0, 1], 2, 2, 16, 64, BF, E4, {}),
+    ([3, 0, 64], [5, 2, 1], 1, 3, 16, 128, HF, E4, {}),
+    # split sequences, of very different lengths
+    ([2000, 1, 700, 3333], [1, 1, 1, 1], 1, 4, 64, 128, BF, E4, {}),
+    ([4097, 0, 130], [1, 1, 1], 2, 1, 16, 64, HF, E5, dict(window=1500)),
+    ([2500, 40], [9, 3], 1, 2, 32, 256, BF, E5, {}),
+    # a longest length that the caller put too low
+    ([3000, 500], [1, 1], 1, 2, 64, 64, BF, E4, dict(max_len=600)),
+    ([900], [1], 1, 1, 64, 64, BF, E4, dict(max_len=1)),
+    # sharp and flat softmax, negative scale
+    ([600, 333], [1, 1], 2, 4, 64, 128, BF, E4, dict(spread=20.0)),
+    ([600, 333], [1, 5], 2, 4, 64, 128, HF, E4, dict(spread=0.01)),
+    ([300], [2], 1, 4, 64, 64, BF, E4, dict(scale=-0.3)),
+]
+
+
+@pytest.mark.parametrize("lens,new,heads,group,bt,dim,dt,fmt,more", ATTENDS)
+def test_attention(wm, lens, new, heads, group, bt, dim, dt, fmt, more):
+    check_attend(wm, lens, new, heads, group, bt, dim, dt, fmt, **more)
+
+
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("window", [0, 40])
+def test_what_is_not_seen_does_not_count(wm, fmt, window):
+    """NaN (and infinite) codes behind the last token and before the window,
+    NaN scales of blocks that no row sees."""
+    bt, lens, new = 16, [37, 130, 64], [5, 1, 3]
+
+    def poison(k, v, ks, vs, rows):
+        bad = 0x7F if fmt == E4 else 0x7C
+        used = {rows[r][j] for r, n in enumerate(lens) for j in range(-(-n // bt))}
+        for t in (ks, vs):
+            for b in range(t.shape[0]):
+                if b not in used:
+                    t[b] = math.nan
+        for r, n in enumerate(lens):
+            blk, off = rows[r][(n - 1) // bt], (n - 1) % bt + 1
+            k.view(torch.uint8)[blk, :, off:] = bad
+            v.view(torch.uint8)[blk, :, :, off:] = bad
+            if window:
+                p = n - new[r]  # the first row's position: nothing sees p - window
+                for j in range(0, max(0, p - window + 1)):
+                    k.view(torch.uint8)[rows[r][j // bt], :, j % bt] = 0xFF
+                    v.view(torch.uint8)[rows[r][j // bt], :, :, j % bt] = 0xFF
+    check_attend(wm, lens, new, 2, 2, bt, 64, BF, fmt, window=window, tail=poison)
+
+
+def test_special_values_reach_the_rows_that_see_them(wm):
+    """A NaN value at token 9 and an infinity at token 12: earlier rows of the
+    same tile are untouched."""
+    bt, lens, new, dim = 16, [20], [20], 64
+    rows, blocks = layout(lens, bt, 3)
+    k, v, ks, vs = make_cache(blocks, 1, bt, dim, E5, 4)
+    v.view(torch.uint8)[rows[0][0], 0, 5, 9] = 0x7F
+    v.view(torch.uint8)[rows[0][0], 0, 6, 12] = 0x7C
+    v.view(torch.uint8)[rows[0][0], 0, 7, 12] = 0xFC
+    v.view(torch.uint8)[rows[0][0], 0, 8, 12] = 0x7C
+    v.view(torch.uint8)[rows[0][0], 0, 8, 13] = 0xFC
+    k.view(torch.uint8)[rows[0][1], 0, 1, 3] = 0x7F  # a NaN key: token 17
+    q = torch.randn(20, 2, dim).to(BF).cuda()
+    out = torch.zeros_like(q)
+    wm.cache_attend(q, k, v, ks, vs, dev(rows), dev(lens), dev([0, 20]), out, max_len=20,
+                    scale=0.1)
+    o = out.float().cpu()
+    assert bool(torch.isfinite(o[:9]).all())
+    assert bool(o[9:, :, 5].isnan().all())
+    assert bool(torch.isfinite(o[9:12][..., [0, 6, 7, 8]]).all())
+    assert bool((o[12:17, :, 6] == math.inf).all()) and bool((o[12:17, :, 7] == -math.inf).all())
+    assert bool((o[12, :, 8] == math.inf).all()) and bool(o[13:17, :, 8].isnan().all())
+    assert bool(torch.isfinite(o[12:17][..., 9:]).all())
+    assert bool(o[17:].isnan().all())
+
+
+def test_blocks_outside_the_pool_count_as_unseen(wm):
+    bt, lens, new = 16, [90, 40], [1, 3]
+    rows, blocks = layout(lens, bt, 5)
+    k, v, ks, vs = make_cache(blocks, 2, bt, 64, E4, 6)
+    q = torch.randn(4, 2, 64).to(BF).cuda()
+    rows[0][2], rows[1][0] = blocks, -1
+    lse, out, verdict = torch.zeros(4, 2, device="cuda"), torch.zeros_like(q), word()
+    wm.cache_attend(q, k, v, ks, vs, dev(rows), dev(lens), dev([0, 1, 4]), out, max_len=90,
+                    scale=0.2, lse=lse, verdict=verdict)
+    assert verdict.item() == 8
+    hidden = lambda r, j: (r, j // bt) in ((0, 2), (1, 0))  # noqa: E731
+    want, z, weight, sp = ref.attend(q.cpu(), values(k, ks, False), values(v, vs, True), rows,
+                                     lens, [0, 1, 4], bt, 0.2, hidden=hidden)
+    bo, bl = ref.attend_bound(BF, want, z, weight, sp, 90, 64)
+    assert bool(((out.cpu().double() - want).abs() <= bo).all())
+    assert bool(((lse.cpu().double() - z).abs() <= bl).all())
+
+
+def test_lengths_beyond_the_table(wm):
+    bt = 16
+    rows, blocks = layout([64], bt, 7)
+    k, v, ks, vs = make_cache(blocks, 1, bt, 64, E4, 8)
+    q = torch.randn(1, 1, 64).to(BF).cuda()
+    a, b, verdict = torch.zeros_like(q), torch.zeros_like(q), word()
+    wm.cache_attend(q, k, v, ks, vs, dev(rows), dev([64]), dev([0, 1]), a, max_len=64, scale=0.2)
+    wm.cache_attend(q, k, v, ks, vs, dev(rows), dev([1 << 30]), dev([0, 1]), b, max_len=64,
+                    scale=0.2, verdict=verdict)
+    assert verdict.item() == 1 and torch.equal(a, b)
+
+
+def test_answers_do_not_depend_on_the_blocks(wm):
+    bt, n, heads, dim = 16, 1900, 2, 64
+    need = -(-n // bt)
+    k, v, ks, vs = make_cache(2 * need, heads, bt, dim, E4, 9)
+    q = torch.randn(1, 8, dim).to(BF).cuda()
+    first = torch.randperm(2 * need)[:need]
+    second = torch.tensor([b for b in range(2 * need) if b not in set(first.tolist())][:need])
+    for t in (k.view(torch.uint8), v.view(torch.uint8), ks, vs):
+        t[second.flip(0).cuda()] = t[first.cuda()].clone()
+    outs = []
+    for ids in (first, second.flip(0)):
+        out = torch.zeros_like(q)
+        ws = torch.empty(wm.attend_ws_bytes(q, k, dev([n]), n), dtype=torch.uint8, device="cuda")
+        wm.cache_attend(q, k, v, ks, vs, dev(ids)[None], dev([n]), dev([0, 1]), out, ws,
+                        max_len=n, scale=0.125)
+        outs.append(out)
+    assert torch.equal(*outs) and bool(outs[0].any())
+
+
+def test_unaligned_queries_and_outputs(wm):
+    bt, lens = 16, [70]
+    rows, blocks = layout(lens, bt, 11)
+    k, v, ks, vs = make_cache(blocks, 1, bt, 64, E4, 12)
+    flat = torch.randn(2 * 67 + 1).to(BF).cuda()
+    q = flat[1:].as_strided((1, 2, 64), (134, 67, 1))
+    aligned, odd = torch.zeros(1, 2, 64, dtype=BF, device="cuda"), torch.zeros(140, dtype=BF,
+                                                                              device="cuda")
+    view = odd[1:].as_strided((1, 2, 64), (134, 67, 1))
+    args = (k, v, ks, vs, dev(rows), dev(lens), dev([0, 1]))
+    wm.cache_attend(q.contiguous(), *args, aligned, max_len=70, scale=0.2)
+    wm.cache_attend(q, *args, view, max_len=70, scale=0.2)
+    assert torch.equal(view, aligned) and bool(aligned.any())
+    odd[1:].as_strided((2, 64), (67, 1)).zero_()
+    assert not odd.any()
+
+
+# ---- blocks and the flat state -----------------------------------------------------
+
+
+def pools_of(shapes, seed):
+    """Pools [blocks, stride bytes] of which each page's first bytes count."""
+    out = []
+    for i, (blocks, page, stride) in enumerate(shapes):
+        out.append(random_bytes(blocks * stride, seed + i).view(blocks, stride)[:, :page])
+    return out
+
+
+POOLS = [
+    ([(5, 4, 4)], 3), ([(9, 4096, 4096), (11, 20, 36)], 7), ([(4, 16384 * 3 + 16, 60000)], 4),
+    ([(40, 3584, 3584), (40, 65536, 65552), (44, 100, 100)], 33),
+    ([(6, 48, 64)] * 70 + [(8, 12, 16)] * 61, 5), ([(3, 8, 8)], 1),
+]
+
+
+@pytest.mark.parametrize("shapes,n", POOLS)
+def test_pages_out_and_in(wm, shapes, n):
+    say(f"[pages] {shapes[:3]} x{len(shapes)} n={n}")
+    pools = pools_of(shapes, 1)
+    blocks = min(s[0] for s in shapes)
+    pages = torch.randperm(blocks, generator=torch.Generator().manual_seed(2))[:min(n, blocks)]
+    want = []
+    for p in pools:
+        b = p[pages.cuda()].reshape(-1)
+        want += [b, torch.zeros(-b.numel() % 16, dtype=torch.uint8, device="cuda")]
+    want = torch.cat(want)
+    total = wm.flat_pages_bytes(pools, pages.numel())
+    assert total == want.numel()
+    flat = torch.full((total + 64,), 0xEE, dtype=torch.uint8, device="cuda")
+    verdict = word()
+    wm.flatten_pages(pools, dev(pages), flat, verdict)
+    assert verdict.item() == 0
+    assert torch.equal(flat[:total], want) and bool((flat[total:] == 0xEE).all())
+    # into other pools' other pages; everything else stays
+    dest = pools_of(shapes, 100)
+    expect = [p.clone() for p in dest]
+    to = pages.flip(0)
+    at = 0
+    for p, e in zip(pools, expect):
+        e[to.cuda()] = p[pages.cuda()]
+        at += p.shape[1]
+    full = [d.as_strided((d.shape[0], d.stride(0)), (d.stride(0), 1)) for d in dest]
+    gaps = [f[:, d.shape[1]:].clone() for f, d in zip(full, dest)]
+    wm.rehydrate_pages(flat, dest, dev(to), verdict)
+    assert verdict.item() == 0
+    for d, e, f, gp in zip(dest, expect, full, gaps):
+        assert torch.equal(d, e) and torch.equal(f[:, d.shape[1]:], gp)
+
+
+def test_pages_move_only_on_a_zero_verdict_and_good_blocks(wm):
+    pools = pools_of([(6, 64, 64), (5, 32, 32)], 3)
+    before = [p.clone() for p in pools]
+    flat = torch.full((1024,), 0x11, dtype=torch.uint8, device="cuda")
+    for pages, v0, v1 in (([0, 1], 4, 4), ([0, 5], 0, 8), ([-1, 1], 0, 8), ([3, 1 << 30], 2, 10)):
+        verdict = dev([v0])
+        wm.rehydrate_pages(flat, pools, dev(pages), verdict)
+        assert verdict.item() == v1
+        verdict = dev([v0])
+        wm.flatten_pages(pools, dev(pages), flat, verdict)
+        assert verdict.item() == v1
+        assert bool((flat == 0x11).all())
+    assert all(torch.equal(a, b) for a, b in zip(pools, before))
+    many = dev([0] * 5000 + [5])
+    big = torch.full((wm.flat_pages_bytes(pools, 5001),), 0x11, dtype=torch.uint8, device="cuda")
+    verdict = word()
+    wm.flatten_pages(pools, many, big, verdict)
+    assert verdict.item() == 8 and bool((big == 0x11).all())
+
+
+# ---- together -----------------------------------------------------------------------
+
+
+def feed(cache, tokens, group, g):
+    """One step's random keys, values and queries through every layer."""
+    outs = []
+    for n in range(cache.layers):
+        k, v = (torch.randn(tokens, cache.heads, cache.dim, generator=g, device="cuda").to(BF)
+                for _ in range(2))
+        q = torch.randn(tokens, cache.heads * group, cache.dim, generator=g,
+                        device="cuda").to(BF)
+        cache.append(n, k, v)
+        outs.append(cache.attend(n, q, 1 / math.sqrt(cache.dim)))
+    return outs
+
+
+def test_a_session_moves_and_answers_the_same():
+    """Prompts, steps, a session's move through the mover (encode, decode,
+    verify, install) into another cache, and the next token there: the same
+    bits as the next token here."""
+    from paper_2607_10389_amd import WM_OK, Mover, PagedCache
+    args = dict(layers=3, heads=2, dim=64, block_tokens=16, max_requests=4)
+    src, dst = PagedCache(blocks=40, **args), PagedCache(blocks=50, **args)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    feed(src, src.step({0: 37, 1: 100, 3: 5}), 4, g)
+    for i in range(20):
+        feed(src, src.step({0: 38 + i, 3: 6 + i}), 4, g)
+    feed(src, src.step({1: 0, 0: 58}), 4, g)  # one leaves, its blocks are reused
+    feed(dst, dst.step({2: 77, 0: 3}), 4, g)  # the destination serves others
+    n = src.lengths[0]
+    flat = src.suspend(0)
+    m = Mover(flat.numel())
+    m.encode_step(flat, None)
+    m.decode()
+    dst.resume(1, n, m.staging, m.verdict)
+    assert m.commit(None, scatter=False) == WM_OK
+    assert int(m.verdict.item()) == 0
+    assert torch.equal(dst.suspend(1), flat)
+    a, b = (torch.Generator(device="cuda").manual_seed(5) for _ in range(2))
+    here = feed(src, src.step({0: n + 1}), 4, a)
+    there = feed(dst, dst.step({1: n + 1}), 4, b)
+    assert all(torch.equal(x, y) and bool(x.any()) for x, y in zip(here, there))
+    # a verdict that is not zero installs nothing
+    dst.step({1: 0})
+    before = dst.codes.clone()
+    dst.resume(1, n, m.staging, dev([4]))
+    assert torch.equal(dst.codes, before)
+
+
+def test_a_step_that_does_not_fit_changes_nothing():
+    from paper_2607_10389_amd import PagedCache, WmError
+    c = PagedCache(layers=1, blocks=4, heads=1, dim=64, block_tokens=16, max_requests=3)
+    c.step({0: 20, 1: 3})
+    before = [t.clone() for t in (c.block_table, c.ring, c.pool, c.lens)]
+    with pytest.raises(WmError):
+        c.step({0: 40, 2: 16})
+    assert all(torch.equal(a, b) for a, b in zip(before, (c.block_table, c.ring, c.pool, c.lens)))
+    assert c.step({0: 0, 1: 16}) == 13 and c.step({2: 48}) == 48
+    with pytest.raises(ValueError):
+        c.resume(2, 5, torch.zeros(1 << 16, dtype=torch.uint8, device="cuda"))
+
+
+def test_captured_step_replays(wm):
+    """Tables, store and attention of a decoding step in one graph, replayed
+    with new lengths and inputs and checked against the eager calls each
+    time; the calls are also made on a stream of their own."""
+    heads, group, bt, dim, n = 2, 4, 16, 64, 3
+    rows, blocks = layout([200] * n, bt, 1, extra=50)
+    free = sorted(set(range(blocks)) - {b for r in rows for b in r})
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, E4, 2)
+    eager = [t.clone() for t in (k.view(torch.uint8), v.view(torch.uint8), ks, vs)]
+    ek, ev, eks, evs = eager[0].view(E4), eager[1].view(E4), eager[2], eager[3]
+    lens, nxt = dev([30, 64, 111]), dev([31, 65, 112])
+    table, ring = dev([r + [0] * 4 for r in rows]), dev(free)
+    pi, po, sl, qs, vd = dev([3, 50]), dev([0, 0]), dev([0] * n, torch.int64), dev([0] * 4), word()
+    x = torch.zeros(n, heads * (group + 2), dim, dtype=BF, device="cuda")
+    q, kn, vn = x[:, :heads * group], x[:, heads * group:heads * (group + 1)], \
+        x[:, heads * (group + 1):]
+    out, lse = torch.zeros(n, heads * group, dim, dtype=BF, device="cuda"), \
+        torch.zeros(n, heads * group, device="cuda")
+    ws = torch.empty(wm.attend_ws_bytes(q, k, nxt, 4000), dtype=torch.uint8, device="cuda")
+
+    def step(kc, vc, s0, s1, o, z, stream=None):
+        wm.page_tables(lens, nxt, bt, table, ring, pi, po, sl, qs, vd, stream)
+        wm.cache_append(kn, vn, kc, vc, s0, s1, sl, qs, None, stream)
+        wm.cache_attend(q, kc, vc, s0, s1, table, nxt, qs, o, ws, max_len=4000, scale=0.125,
+                        lse=z, stream=stream)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(ek, ev, eks, evs, torch.zeros_like(out), torch.zeros_like(lse), side)
+    side.synchronize()
+    for a, b in zip(eager, (k.view(torch.uint8), v.view(torch.uint8), ks, vs)):
+        a.copy_(b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(k, v, ks, vs, out, lse)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for i in range(6):
+        x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+        graph.replay()
+        want, z = torch.zeros_like(out), torch.zeros_like(lse)
+        step(ek, ev, eks, evs, want, z)
+        torch.cuda.synchronize()
+        assert vd.item() == 0
+        assert torch.equal(out, want) and torch.equal(lse, z) and bool(out.any()), i
+        assert torch.equal(k.view(torch.uint8), eager[0])
+        assert torch.equal(v.view(torch.uint8), eager[1])
+        lens.copy_(nxt)
+        nxt.add_(1)
+        pi.copy_(po)
