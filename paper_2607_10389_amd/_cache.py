@@ -10,6 +10,7 @@ the tensors' device and, without a ``stream``, on its current stream.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -79,68 +80,99 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _vec(t, dtype, dev, name, n=None):
-    """Address of a dense one-dimensional tensor (of at least n entries)."""
-    _need(t.dtype == dtype and t.dim() == 1 and (t.numel() <= 1 or t.stride(0) == 1),
-          f"{name} is a dense vector of {dtype}")
-    _need(t.device == dev, f"{name} is on {t.device}, not on {dev}")
-    _need(n is None or t.numel() >= n, f"{name} has fewer than {n} entries")
-    return t.data_ptr()
+# The checks below are on a decoding step's way, where a call's kernel runs
+# for a few microseconds: each is one expression over the tensor's cheapest
+# properties (a device is its number), and words are made only for an error.
+
+
+def _vec(t, dtype, dev, n, name):
+    """Address of a dense tensor of at least n entries."""
+    if (t.dtype is dtype and t.get_device() == dev and t.numel() >= n and t.is_contiguous()):
+        return t.data_ptr()
+    raise ValueError(f"{name} is a dense {dtype} tensor of at least {n} entries on device {dev}")
 
 
 def _word(t, dev):
     """Address of the verdict word (None -> NULL)."""
     if t is None:
         return None
-    _need(t.dtype in (torch.int32, torch.uint32) and t.numel() >= 1 and t.device == dev,
-          "verdict is a 32-bit word on the same device")
-    return t.data_ptr()
+    if t.get_device() == dev and t.dtype in _WORD and t.numel() >= 1:
+        return t.data_ptr()
+    raise ValueError(f"verdict is a 32-bit word on device {dev}")
 
 
-def _device(t):
-    _need(t.is_cuda, "libwm takes device tensors")
-    return t.device
+_WORD = (torch.int32, torch.uint32)
+
+
+def _device(t) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("libwm takes device tensors")
+    return dev
 
 
 def _run(where, dev, stream, fn, *args):
     """fn(*args, stream) on dev: a stream belongs to a device, and a kernel is
     launched on the current one."""
-    s = stream if stream is not None else torch.cuda.current_stream(dev)
-    _need(s.device == dev, f"the stream is of {s.device}, the tensors are on {dev}")
-    if dev.index == torch.cuda.current_device():
-        return _check(fn(*args, s.cuda_stream), where)
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(dev)
+    else:
+        _need(stream.device.index == dev, f"the stream is of {stream.device}, the tensors of {dev}")
+        s = stream.cuda_stream
+    if dev == torch._C._cuda_getDevice():
+        return _check(fn(*args, s), where)
     with torch.cuda.device(dev):
-        return _check(fn(*args, s.cuda_stream), where)
+        return _check(fn(*args, s), where)
+
+
+_pack_cache = struct.Struct("=8Q6I").pack
+_pack_rows = struct.Struct("=3Q2I").pack
 
 
 def cache_desc(k_cache, v_cache, k_scale, v_scale) -> Cache:
     """The library's description of one layer's cache."""
     dev = _device(k_cache)
-    _need(k_cache.dtype in _FORMAT and v_cache.dtype == k_cache.dtype,
-          "key and value codes are of one 8-bit float type")
-    _need(k_cache.dim() == 4 and v_cache.dim() == 4, "codes are [blocks, heads, .., ..]")
+    _need(k_cache.dim() == 4, "codes are [blocks, heads, .., ..]")
     n, h, bt, d = k_cache.shape
-    _need(v_cache.shape == (n, h, d, bt), "value codes are [blocks, heads, dim, block_tokens]")
-    ks, vs = k_cache.stride(), v_cache.stride()
-    _need((h == 1 or (ks[1] == bt * d and vs[1] == bt * d)) and ks[2] == d and vs[2] == bt
-          and ks[3] == 1 and vs[3] == 1, "a block's codes are dense")
-    for s in (k_scale, v_scale):
-        _need(s.dtype == torch.float32 and s.shape == (n, h) and (h == 1 or s.stride(1) == 1),
-              "scales are float32 [blocks, heads], dense within a block")
-    _need(v_cache.device == dev and k_scale.device == dev and v_scale.device == dev,
-          "a cache's tensors are on one device")
+    ks, vs, fmt = k_cache.stride(), v_cache.stride(), _FORMAT.get(k_cache.dtype)
+    if fmt is None or v_cache.dtype is not k_cache.dtype:
+        raise ValueError("key and value codes are of one 8-bit float type")
+    if v_cache.shape != (n, h, d, bt):
+        raise ValueError("value codes are [blocks, heads, dim, block_tokens]")
+    dense = ks[2] == d and vs[2] == bt and ks[3] == 1 and vs[3] == 1
+    if not dense or (h > 1 and (ks[1] != bt * d or vs[1] != bt * d)):
+        raise ValueError("a block's codes are dense")
+    k_step, v_step = k_scale.stride(), v_scale.stride()
+    for s, step in ((k_scale, k_step), (v_scale, v_step)):
+        if s.dtype is not torch.float32 or s.shape != (n, h) or (h > 1 and step[1] != 1):
+            raise ValueError("scales are float32 [blocks, heads], dense within a block")
+    if not dev == v_cache.get_device() == k_scale.get_device() == v_scale.get_device():
+        raise ValueError("a cache's tensors are on one device")
     one = n == 1  # the stride of a single block says nothing
-    return Cache(k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
-                 h * bt * d if one else ks[0], h * bt * d if one else vs[0],
-                 h if one else k_scale.stride(0), h if one else v_scale.stride(0),
-                 n, h, bt, d, _FORMAT[k_cache.dtype], 0)
+    page = h * bt * d
+    return Cache.from_buffer_copy(_pack_cache(
+        k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+        page if one else ks[0], page if one else vs[0], h if one else k_step[0],
+        h if one else v_step[0], n, h, bt, d, fmt, 0))
 
 
-def _rows(t, heads, dim, name) -> Rows:
-    _need(t.dtype in _DTYPE and t.dim() == 3 and t.shape[1] == heads and t.shape[2] == dim
-          and t.stride(2) == 1, f"{name} is [tokens, {heads}, {dim}] of bfloat16 or float16, "
-          "its vectors dense")
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1), _DTYPE[t.dtype], 0)
+def _rows(t, heads, dim, dev, name) -> Rows:
+    dt, shape, step = _DTYPE.get(t.dtype), t.shape, t.stride()
+    if (dt is None or len(shape) != 3 or shape[1] != heads or shape[2] != dim or step[2] != 1
+            or t.get_device() != dev):
+        raise ValueError(f"{name} is [tokens, {heads}, {dim}] of bfloat16 or float16 on device "
+                         f"{dev}, its vectors dense")
+    return Rows.from_buffer_copy(_pack_rows(t.data_ptr(), step[0], step[1], dt, 0))
+
+
+def _table(t, n, dev):
+    """(address, row stride, width) of a block table of at least n rows."""
+    step = t.stride()
+    if (t.dtype is not torch.int32 or len(step) != 2 or t.shape[0] < n
+            or (step[1] != 1 and t.shape[1] > 1) or t.get_device() != dev):
+        raise ValueError(f"block_table is int32 [requests, max_blocks] on device {dev}")
+    width = t.shape[1]
+    return t.data_ptr(), step[0] if t.shape[0] > 1 else width, width
 
 
 def page_tables(old_len, new_len, block_tokens, block_table, free_ring, pool_in, pool_out,
@@ -150,18 +182,13 @@ def page_tables(old_len, new_len, block_tokens, block_table, free_ring, pool_in,
     [requests, max_blocks], free_ring the ring of free blocks, pool_in and
     pool_out {first place, count}; slot_map is int64, the rest int32."""
     dev, i32, n = _device(old_len), torch.int32, old_len.numel()
-    _need(block_table.dtype == i32 and block_table.dim() == 2 and block_table.shape[0] >= n
-          and (block_table.shape[1] <= 1 or block_table.stride(1) == 1)
-          and block_table.device == dev, "block_table is int32 [requests, max_blocks]")
-    width = block_table.shape[1]
-    stride = block_table.stride(0) if block_table.shape[0] > 1 else width
     return _run("wm_page_tables", dev, stream, LIB.wm_page_tables,
-                _vec(old_len, i32, dev, "old_len"), _vec(new_len, i32, dev, "new_len", n), n,
-                block_tokens, block_table.data_ptr(), stride, width,
-                _vec(free_ring, i32, dev, "free_ring"), free_ring.numel(),
-                _vec(pool_in, i32, dev, "pool_in", 2), _vec(pool_out, i32, dev, "pool_out", 2),
-                _vec(slot_map, torch.int64, dev, "slot_map"), slot_map.numel(),
-                _vec(q_start, i32, dev, "q_start", n + 1), _word(verdict, dev))
+                _vec(old_len, i32, dev, n, "old_len"), _vec(new_len, i32, dev, n, "new_len"), n,
+                block_tokens, *_table(block_table, n, dev),
+                _vec(free_ring, i32, dev, 1, "free_ring"), free_ring.numel(),
+                _vec(pool_in, i32, dev, 2, "pool_in"), _vec(pool_out, i32, dev, 2, "pool_out"),
+                _vec(slot_map, torch.int64, dev, 0, "slot_map"), slot_map.numel(),
+                _vec(q_start, i32, dev, n + 1, "q_start"), _word(verdict, dev))
 
 
 def cache_append(k, v, k_cache, v_cache, k_scale, v_scale, slot_map, q_start, verdict=None,
@@ -169,14 +196,13 @@ def cache_append(k, v, k_cache, v_cache, k_scale, v_scale, slot_map, q_start, ve
     """Store new keys and values [tokens, heads, dim] where slot_map says
     (wm_cache_append); q_start has an entry per request and one more."""
     c = cache_desc(k_cache, v_cache, k_scale, v_scale)
-    dev, n = k_cache.device, k.shape[0]
-    kr, vr = _rows(k, c.n_heads, c.head_dim, "k"), _rows(v, c.n_heads, c.head_dim, "v")
-    _need(v.shape[0] == n and v.dtype == k.dtype and k.device == dev and v.device == dev,
-          "k and v have the same tokens, type and device as the cache")
-    _need(q_start.numel() >= 1, "q_start has an entry per request and one more")
+    dev, n, h, d = k_cache.get_device(), k.shape[0], k_cache.shape[1], k_cache.shape[3]
+    kr, vr = _rows(k, h, d, dev, "k"), _rows(v, h, d, dev, "v")
+    if v.shape[0] != n or v.dtype is not k.dtype:
+        raise ValueError("k and v have the same tokens and type")
+    starts = _vec(q_start, torch.int32, dev, 1, "q_start")
     return _run("wm_cache_append", dev, stream, LIB.wm_cache_append, c, kr, vr,
-                _vec(slot_map, torch.int64, dev, "slot_map", n),
-                _vec(q_start, torch.int32, dev, "q_start"), q_start.numel() - 1, n,
+                _vec(slot_map, torch.int64, dev, n, "slot_map"), starts, q_start.numel() - 1, n,
                 _word(verdict, dev))
 
 
@@ -194,27 +220,18 @@ def cache_attend(q, k_cache, v_cache, k_scale, v_scale, block_table, lens, q_sta
     (wm_cache_attend).  lens counts the new tokens; ws holds at least
     attend_ws_bytes()."""
     c = cache_desc(k_cache, v_cache, k_scale, v_scale)
-    dev, i32, n = k_cache.device, torch.int32, q.shape[0]
-    hq = q.shape[1] if q.dim() == 3 else 0
-    qr, outr = _rows(q, hq, c.head_dim, "q"), _rows(out, hq, c.head_dim, "out")
-    _need(out.shape[0] == n and out.dtype == q.dtype and q.device == dev and out.device == dev,
-          "out has the tokens, type and device of q")
+    dev, i32 = k_cache.get_device(), torch.int32
+    n, hq, d = q.shape
+    qr, outr = _rows(q, hq, k_cache.shape[3], dev, "q"), _rows(out, hq, d, dev, "out")
+    if out.shape[0] != n or out.dtype is not q.dtype:
+        raise ValueError("out has the tokens and type of q")
     n_req = lens.numel()
-    _need(block_table.dtype == i32 and block_table.dim() == 2 and block_table.shape[0] >= n_req
-          and (block_table.shape[1] <= 1 or block_table.stride(1) == 1)
-          and block_table.device == dev, "block_table is int32 [requests, max_blocks]")
-    width = block_table.shape[1]
-    stride = block_table.stride(0) if block_table.shape[0] > 1 else width
-    if lse is not None:
-        _need(lse.dtype == torch.float32 and lse.shape == (n, hq) and lse.is_contiguous()
-              and lse.device == dev, "lse is dense float32 [tokens, query heads]")
-    if ws is not None:
-        _need(ws.device == dev and ws.is_contiguous(), "ws is a dense tensor on the same device")
     return _run("wm_cache_attend", dev, stream, LIB.wm_cache_attend, c, qr, outr,
-                None if lse is None else lse.data_ptr(), hq, block_table.data_ptr(), stride,
-                width, _vec(lens, i32, dev, "lens"),
-                _vec(q_start, i32, dev, "q_start", n_req + 1), n_req, n, max_len, scale, window,
-                _word(verdict, dev), None if ws is None else ws.data_ptr(),
+                None if lse is None else _vec(lse, torch.float32, dev, n * hq, "lse"), hq,
+                *_table(block_table, n_req, dev), _vec(lens, i32, dev, 0, "lens"),
+                _vec(q_start, i32, dev, n_req + 1, "q_start"), n_req, n, max_len, scale, window,
+                _word(verdict, dev),
+                None if ws is None else _vec(ws, ws.dtype, dev, 0, "ws"),
                 0 if ws is None else ws.numel() * ws.element_size())
 
 
@@ -228,8 +245,8 @@ class PoolTable:
         self.t = (Pool * max(self.n, 1))()
         self.device = _device(pools[0]) if self.n else None
         for i, x in enumerate(pools):
-            _need(x.is_cuda and x.dim() >= 1 and x.shape[0] > 0 and x[0].is_contiguous()
-                  and x.device == self.device,
+            _need(x.dim() >= 1 and x.shape[0] > 0 and x[0].is_contiguous()
+                  and x.get_device() == self.device,
                   "pools are device tensors [blocks, ...] with dense pages")
             page = x[0].numel() * x.element_size()
             self.t[i].ptr, self.t[i].page_bytes = x.data_ptr(), page
@@ -251,7 +268,7 @@ def flatten_pages(pools, pages, flat, verdict, stream=None):
     tab, dev = _pools(pools), _device(flat)
     _need(tab.device in (None, dev) and flat.is_contiguous(), "flat is dense, on the pools' device")
     return _run("wm_flatten_pages", dev, stream, LIB.wm_flatten_pages, tab.t, tab.n,
-                _vec(pages, torch.int32, dev, "pages"), pages.numel(), flat.data_ptr(),
+                _vec(pages, torch.int32, dev, 0, "pages"), pages.numel(), flat.data_ptr(),
                 flat.numel() * flat.element_size(), _word(verdict, dev))
 
 
@@ -261,4 +278,4 @@ def rehydrate_pages(flat, pools, pages, verdict, stream=None):
     _need(tab.device in (None, dev) and flat.is_contiguous(), "flat is dense, on the pools' device")
     return _run("wm_rehydrate_pages", dev, stream, LIB.wm_rehydrate_pages, flat.data_ptr(),
                 flat.numel() * flat.element_size(), tab.t, tab.n,
-                _vec(pages, torch.int32, dev, "pages"), pages.numel(), _word(verdict, dev))
+                _vec(pages, torch.int32, dev, 0, "pages"), pages.numel(), _word(verdict, dev))

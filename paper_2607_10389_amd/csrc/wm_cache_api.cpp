@@ -120,20 +120,14 @@ namespace wm {
 
 AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
                        uint32_t n_q_heads, uint32_t head_dim, uint32_t max_len) {
-  AttendPlan p = {16, 1, 1, 1};
+  AttendPlan p = {16, 1, 1};
   if (!n_requests || !n_tokens || !n_heads || n_q_heads < n_heads) return p;
   const uint64_t rows = (uint64_t)n_tokens * (n_q_heads / n_heads);
   (void)head_dim;
   if (rows > 16ull * n_requests) p.rows = 32;
   p.tiles = (uint32_t)(rows / p.rows + n_requests);
-  const uint64_t wgs = std::max<uint64_t>(rows / p.rows, n_requests) * n_heads;
-  const uint64_t steps = std::max<uint64_t>(1, (max_len + 63ull) / 64);
-  const uint64_t want = std::min<uint64_t>((2048 + wgs - 1) / wgs, (steps + 7) / 8);
-  uint64_t per = (steps + want - 1) / want;
-  if (want > 1) per = std::min<uint64_t>(per, 128);
-  per = std::max(per, (steps + 65534) / 65535);  // the grid's third axis
-  p.steps = (uint32_t)per;
-  p.splits = (uint32_t)((steps + per - 1) / per);
+  // parts of 512 tokens, or of more so that there are at most 32
+  p.splits = (uint32_t)std::min<uint64_t>(32, std::max<uint64_t>(1, (max_len + 511ull) / 512));
   return p;
 }
 
@@ -251,6 +245,8 @@ wm_status wm_cache_attend(const wm_cache *cache, const wm_rows *q, const wm_rows
   a.group = n_q_heads / cache->n_heads;
   a.max_blocks = max_blocks;
   a.window = window;
+  a.n_cu = (uint32_t)cus();
+  if (!a.n_cu) return WM_ERR_HIP;
   a.scale_log2 = (float)((double)scale * 1.4426950408889634);
   return hip_status(launch_cache_attend(a, stream));
 }

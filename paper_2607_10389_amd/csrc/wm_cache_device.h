@@ -56,9 +56,10 @@ struct Code;
 template <>
 struct Code<WM_E4M3> {
   static constexpr float kLargest = 448.0f;
-  // codes with no finite value: the NaN of either sign
-  static __device__ __forceinline__ bool special(uint32_t b) { return (b & 0x7Fu) == 0x7Fu; }
-  static __device__ __forceinline__ bool infinite(uint32_t) { return false; }
+  // bit 7 of each byte that is a code with no finite value: the NaN of either sign
+  static __device__ __forceinline__ uint32_t special(uint32_t w) {
+    return (w & 0x7F7F7F7Fu) + 0x01010101u;
+  }
   static __device__ __forceinline__ uint32_t two(float x, float y) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xFFFFu;
   }
@@ -78,8 +79,9 @@ struct Code<WM_E4M3> {
 template <>
 struct Code<WM_E5M2> {
   static constexpr float kLargest = 57344.0f;
-  static __device__ __forceinline__ bool special(uint32_t b) { return (b & 0x7Fu) >= 0x7Cu; }
-  static __device__ __forceinline__ bool infinite(uint32_t b) { return (b & 0x7Fu) == 0x7Cu; }
+  static __device__ __forceinline__ uint32_t special(uint32_t w) {
+    return (w & 0x7F7F7F7Fu) + 0x04040404u;  // infinities too
+  }
   static __device__ __forceinline__ uint32_t two(float x, float y) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(x, y, 0, false) & 0xFFFFu;
   }
@@ -105,52 +107,88 @@ __device__ __forceinline__ float load_elem(const void *p, uint64_t i) {
 
 // ---- attention ----------------------------------------------------------------
 
-// Tiles.  A request's query rows that share a key head are its tokens times the
-// heads of the group, row = token * group + head; a tile is 16 NQ of them.
-struct Tile {
-  uint32_t r, row0, n_rows;  // request, its first row, its rows in all
-  int64_t q0;                // its first token
-  int32_t len, pos0;         // its length, position of its first new token
-  uint32_t lo, hi;           // tokens that some row of the tile sees: [lo, hi)
+// A request as attention sees it.  Its query rows that share a key head are its
+// tokens times the heads of the group, row = token * group + head; tiles of
+// `rows` of them are worked on together.  Its sequence is cut into parts of 2^cut tokens
+// (512, or more where the span that some row sees has over 30 of them), at
+// multiples of that: the cut depends on the request alone, so a request of
+// one tile gives the same bits whatever else the call holds.
+struct Request {
+  int64_t q0;             // its first query row's token
+  uint32_t n_rows, tiles;
+  int32_t len, pos0;      // its length, position of its first new token
+  uint32_t cut, part0, parts;
 };
 
-__device__ __forceinline__ bool tile_of(const AttendArgs &a, uint32_t place, Tile *t) {
-  const uint32_t rows = a.plan.rows;
-  const Places pl = {a.q_start, a.n_requests, a.group, rows, 1u};
-  const uint32_t r = __builtin_amdgcn_readfirstlane(pl.find(place));
-  int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1];
+__device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, bool tell) {
+  Request x = {0, 0, 0, 0, 0, 9, 0, 1};
+  int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1], len = a.len[r];
   q0 = q0 > 0 ? q0 : 0;
   q1 = q1 < (int64_t)a.n_tokens ? q1 : (int64_t)a.n_tokens;
-  const int64_t nth = (int64_t)place - pl.first(r);
-  if (nth < 0 || q0 >= q1) return false;
-  const uint64_t n_rows = (uint64_t)(q1 - q0) * a.group;
-  if ((uint64_t)nth * rows >= n_rows) return false;
+  if (q0 >= q1) return x;
   const int64_t cap = (int64_t)a.max_blocks << a.bt_log2;
-  int64_t len = a.len[r];
   if (len > cap) {
     len = cap;
-    if (threadIdx.x == 0 && a.verdict) atomicOr(a.verdict, WM_C_LENGTH);
+    if (tell && a.verdict) atomicOr(a.verdict, WM_C_LENGTH);
   }
   len = len > 0 ? len : 0;
-  t->r = r;
-  t->row0 = (uint32_t)nth * rows;
-  t->n_rows = (uint32_t)n_rows;
-  t->q0 = q0;
-  t->len = (int32_t)len;
-  t->pos0 = (int32_t)(len - (q1 - q0));
-  const uint32_t last = t->row0 + rows < t->n_rows ? t->row0 + rows - 1 : t->n_rows - 1;
-  const int64_t p_lo = (int64_t)t->pos0 + t->row0 / a.group;
-  const int64_t p_hi = (int64_t)t->pos0 + last / a.group;
-  int64_t lo = 0;
-  if (a.window && p_lo + 1 > (int64_t)a.window) lo = p_lo + 1 - a.window;
-  t->hi = p_hi + 1 > 0 ? (uint32_t)(p_hi + 1) : 0u;
-  t->lo = (uint32_t)(lo < (int64_t)t->hi ? lo : t->hi);
-  return true;
+  const int64_t p0 = len - (q1 - q0);
+  const uint32_t lo =
+      a.window && p0 + 1 > (int64_t)a.window ? (uint32_t)(p0 + 1 - a.window) : 0u;
+  const uint32_t hi = (uint32_t)len;
+  x.q0 = q0;
+  x.n_rows = (uint32_t)((q1 - q0) * a.group);
+  x.tiles = (x.n_rows + a.plan.rows - 1) / a.plan.rows;
+  x.len = (int32_t)len;
+  x.pos0 = (int32_t)p0;
+  while (((hi - lo) >> x.cut) >= 31u) ++x.cut;
+  auto parts = [&]() { return (uint32_t)(((uint64_t)hi + (1u << x.cut) - 1) >> x.cut) - (lo >> x.cut); };
+  while (parts() > a.plan.splits) ++x.cut;  // longer than the caller's longest
+  x.part0 = lo >> x.cut;
+  x.parts = parts();
+  x.parts = x.parts ? x.parts : 1u;
+  return x;
 }
 
-__device__ __forceinline__ uint32_t splits_of(const AttendArgs &a, const Tile &t) {
-  const uint32_t s0 = t.lo >> 6, s1 = (t.hi + 63u) >> 6;
-  return (s1 - s0 + a.plan.steps - 1) / a.plan.steps;
+// The tokens [lo, hi) that some row of a tile sees, and its parts.
+struct Tile {
+  uint32_t row0, lo, hi, part0, part1;
+};
+
+__device__ __forceinline__ Tile tile_of(const AttendArgs &a, const Request &x, uint32_t i) {
+  Tile t;
+  t.row0 = i * a.plan.rows;
+  const uint32_t last = t.row0 + a.plan.rows < x.n_rows ? t.row0 + a.plan.rows - 1 : x.n_rows - 1;
+  const int64_t p_lo = (int64_t)x.pos0 + t.row0 / a.group;
+  const int64_t p_hi = (int64_t)x.pos0 + last / a.group;
+  const int64_t lo = a.window && p_lo + 1 > (int64_t)a.window ? p_lo + 1 - a.window : 0;
+  t.hi = p_hi + 1 > 0 ? (uint32_t)(p_hi + 1) : 0u;
+  t.lo = (uint32_t)(lo < (int64_t)t.hi ? lo : t.hi);
+  t.part0 = t.lo >> x.cut;
+  t.part1 = (uint32_t)(((uint64_t)t.hi + (1u << x.cut) - 1) >> x.cut);
+  if (t.hi == t.lo) t.part1 = t.part0;
+  return t;
+}
+
+// Where a tile's parts lie in the workspace.
+__device__ __forceinline__ uint64_t part_place(const AttendArgs &a, const Request &x, uint32_t r,
+                                               uint32_t tile, uint32_t part, uint32_t h) {
+  const uint64_t place = (uint64_t)x.q0 * a.group / a.plan.rows + r + tile;
+  return ((place * a.plan.splits + part) * a.c.n_heads + h) * a.plan.rows;
+}
+
+// The same request in every lane of a wave, told to the compiler.
+__device__ __forceinline__ Request uniform(const Request &x) {
+  Request y = x;
+  y.q0 = (int64_t)__builtin_amdgcn_readfirstlane((int)x.q0);  // a row of n_tokens: 31 bits
+  y.n_rows = __builtin_amdgcn_readfirstlane(x.n_rows);
+  y.tiles = __builtin_amdgcn_readfirstlane(x.tiles);
+  y.len = __builtin_amdgcn_readfirstlane(x.len);
+  y.pos0 = __builtin_amdgcn_readfirstlane(x.pos0);
+  y.cut = __builtin_amdgcn_readfirstlane(x.cut);
+  y.part0 = __builtin_amdgcn_readfirstlane(x.part0);
+  y.parts = __builtin_amdgcn_readfirstlane(x.parts);
+  return y;
 }
 
 // Query element types: the key codes are exact in either, so the product with

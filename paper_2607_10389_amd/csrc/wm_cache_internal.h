@@ -32,12 +32,11 @@ struct AppendArgs {
 };
 int launch_cache_append(const AppendArgs &a, void *stream);
 
-// How an attention call is split (a function of host numbers alone).
+// How an attention call is laid out (a function of host numbers alone).
 struct AttendPlan {
-  uint32_t rows;    // query rows (tokens x group) of a tile: 16, 32 or 64
+  uint32_t rows;    // query rows (tokens x group) of a tile
   uint32_t tiles;   // tile places: at least the tiles of every request
-  uint32_t steps;   // 64-token steps of a split
-  uint32_t splits;  // splits of the longest sequence
+  uint32_t splits;  // most parts that a tile's sequence is cut into: 1..32
 };
 AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
                        uint32_t n_q_heads, uint32_t head_dim, uint32_t max_len);
@@ -50,9 +49,9 @@ struct AttendArgs {
   uint64_t table_stride;
   const int32_t *len, *q_start;
   uint32_t *verdict;
-  float *part_out, *part_lse;  // workspace: [tiles][heads][splits][rows] vectors, numbers
+  float *part_out, *part_lse;  // workspace: [tiles][splits][heads][rows] vectors, numbers
   AttendPlan plan;
-  uint32_t n_requests, n_tokens, group, max_blocks, bt_log2, window;
+  uint32_t n_requests, n_tokens, group, max_blocks, bt_log2, window, n_cu;
   float scale_log2;  // scale * log2(e)
 };
 int launch_cache_attend(const AttendArgs &a, void *stream);

@@ -248,47 +248,64 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
 
 // ---- attention: the parts of a split sequence joined ---------------------------
 
-// Joins the splits of a tile: a wave takes one row, its splits in order.
-template <int DT>
-__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a, uint32_t n_split_max) {
-  Tile t;
-  if (!tile_of(a, blockIdx.x, &t)) return;
-  uint32_t n_split = splits_of(a, t);
-  if (n_split <= 1) return;
-  n_split = n_split < n_split_max ? n_split : n_split_max;
-  const uint32_t h = blockIdx.y, D = a.c.head_dim, rows = a.plan.rows;
+// A wave takes one query row: its parts' sums in one load (a lane each), then
+// the weighted sum of the parts in their order.
+template <int DT, int KD>
+__global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
+  const uint32_t hq_all = a.group * a.c.n_heads;
+  const uint64_t at = (uint64_t)blockIdx.x * (kAttThreads / 64) + (threadIdx.x >> 6);
+  const uint64_t token = at / hq_all;
+  if (token >= a.n_tokens) return;
+  const uint32_t hq = (uint32_t)(at - token * hq_all), h = hq / a.group;
+  const Places pl = {a.q_start, a.n_requests, 1u, 1u, 0u};
+  const uint32_t r = __builtin_amdgcn_readfirstlane(pl.find((int64_t)token));
+  const Request x = request_of(a, r, false);
+  if ((int64_t)token < x.q0) return;
+  const uint64_t row = (token - (uint64_t)x.q0) * a.group + (hq - h * a.group);
+  if (row >= x.n_rows) return;
+  const uint32_t tile = (uint32_t)row / a.plan.rows;
+  const Tile t = tile_of(a, x, tile);
+  const uint32_t n = t.part1 - t.part0;
+  if (n <= 1) return;
   const int lane = lane_id();
-  for (uint32_t i = threadIdx.x >> 6; i < rows && t.row0 + i < t.n_rows; i += kAttThreads / 64) {
-    const uint64_t at = (((uint64_t)blockIdx.x * gridDim.y + h) * n_split_max) * rows + i;
-    float top = kNegInf;
-    bool nan = false;
-    for (uint32_t z = 0; z < n_split; ++z) {
-      const float x = a.part_lse[at + (uint64_t)z * rows];
-      nan |= x != x;
-      top = fmaxf(top, x);
+  const uint64_t p0 = part_place(a, x, r, tile, 0, h) + row % a.plan.rows;
+  const uint64_t step = (uint64_t)a.c.n_heads * a.plan.rows;  // from a part to the next
+  const float z = (uint32_t)lane < n ? a.part_lse[p0 + lane * step] : kNegInf;
+  float top = z;
+  for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
+  const float use = top == kNegInf ? 0.0f : top;
+  const float weight = __builtin_amdgcn_exp2f(z - use);
+  float sum = weight;
+  for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
+  // eight parts in flight; a lane has KD neighbouring dimensions
+  float o[KD];
+#pragma unroll
+  for (int j = 0; j < KD; ++j) o[j] = 0.0f;
+  const float *p = a.part_out + p0 * (64 * KD) + lane * KD;
+  for (uint32_t k0 = 0; k0 < n; k0 += 8) {
+    float y[8][KD];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t kk = k0 + k < n ? k0 + k : n - 1;
+#pragma unroll
+      for (int j = 0; j < KD; ++j) y[k][j] = p[kk * step * (64 * KD) + j];
     }
-    const float use = top == kNegInf ? 0.0f : top;
-    float sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t z = 0; z < n_split; ++z) {
-      const uint64_t p = at + (uint64_t)z * rows;
-      const float f = __builtin_amdgcn_exp2f(a.part_lse[p] - use);
-      sum += f;
-      for (uint32_t j = 0; j < D / 64; ++j) {
-        const float x = a.part_out[p * D + 64 * j + lane];
-        o[j] += f == 0.0f ? 0.0f : f * x;  // a split that saw nothing, whatever its part holds
-      }
-    }
-    const uint32_t row = t.row0 + i, tok = row / a.group, hq = h * a.group + row % a.group;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *op = (uint16_t *)a.out.ptr + (uint64_t)(t.q0 + tok) * a.out.row_stride +
-                   (uint64_t)hq * a.out.head_stride;
-    for (uint32_t j = 0; j < D / 64; ++j)
-      op[64 * j + lane] = (uint16_t)Qk<DT, WM_E4M3>::two(nan ? __builtin_nanf("") : o[j] * inv, 0.0f);
-    if (lane == 0 && a.lse) {
-      const float lse2 = nan ? __builtin_nanf("") : (sum == 0.0f ? kNegInf : use + __builtin_amdgcn_logf(sum));
-      a.lse[(uint64_t)(t.q0 + tok) * (a.group * a.c.n_heads) + hq] = lse2 * 0.6931471805599453f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      // a weight of 0 behind the last part
+      const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), k0 + k));
+#pragma unroll
+      for (int j = 0; j < KD; ++j) o[j] += f == 0.0f ? 0.0f : f * y[k][j];
     }
   }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint16_t *op = (uint16_t *)a.out.ptr + token * a.out.row_stride +
+                 (uint64_t)hq * a.out.head_stride + lane * KD;
+#pragma unroll
+  for (int j = 0; j < KD; ++j) op[j] = (uint16_t)Qk<DT, WM_E4M3>::two(o[j] * inv, 0.0f);
+  if (lane == 0 && a.lse)
+    a.lse[token * hq_all + hq] =
+        (sum == 0.0f ? kNegInf : use + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 // ---- a session's blocks and the flat state -----------------------------------
@@ -368,11 +385,20 @@ int launch_cache_attend(const AttendArgs &a, void *stream) {
                      : launch_attend_256(a, stream);
   if (e || a.plan.splits <= 1) return e;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const dim3 grid(a.plan.tiles, a.c.n_heads);
-  if (a.q.dtype == WM_BF16)
-    k_attend_join<WM_BF16><<<grid, kAttThreads, 0, st>>>(a, a.plan.splits);
-  else
-    k_attend_join<WM_FP16><<<grid, kAttThreads, 0, st>>>(a, a.plan.splits);
+  const uint64_t waves = (uint64_t)a.n_tokens * a.group * a.c.n_heads;
+  const uint32_t grid = (uint32_t)((waves + kAttThreads / 64 - 1) / (kAttThreads / 64));
+  const bool bf = a.q.dtype == WM_BF16;
+  switch (d / 64) {
+#define WM_JOIN(kd)                                                      \
+  case kd:                                                               \
+    if (bf)                                                              \
+      k_attend_join<WM_BF16, kd><<<grid, kAttThreads, 0, st>>>(a);       \
+    else                                                                 \
+      k_attend_join<WM_FP16, kd><<<grid, kAttThreads, 0, st>>>(a);       \
+    break;
+    WM_JOIN(1) WM_JOIN(2) WM_JOIN(3) WM_JOIN(4)
+#undef WM_JOIN
+  }
   return last_error();
 }
 
