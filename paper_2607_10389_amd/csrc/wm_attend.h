@@ -21,6 +21,203 @@ struct Rows {
   float vref;          // o is in units of vref 2^-kLift
 };
 
+template <int D, int NQ>
+__device__ __forceinline__ void clear(Rows<D, NQ> *w) {
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    w->m[n] = kNegInf;
+    w->l[n] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) w->o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  w->vref = 0x1p-125f;  // below it a scale has no exact reciprocal
+}
+
+// The maximum over the four lane groups that share a row.
+__device__ __forceinline__ float group_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto p = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const float y = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  const uint32_t v = __float_as_uint(y);
+  const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+// Queries as the first product's right operand (column = row of the tile), the
+// head's dimensions in the order in which the keys' 16-byte loads give them,
+// and the rows' positions (-1: no row).
+template <int DT, int FMT, int D, int NQ>
+__device__ __forceinline__ void load_queries(const AttendArgs &a, const Request &x, uint32_t row0,
+                                             uint32_t h,
+                                             typename Qk<DT, FMT>::frag (&q)[NQ][D / 32],
+                                             int (&pos)[NQ]) {
+  typedef typename Qk<DT, FMT>::frag frag;
+  const int lane = lane_id(), c16 = lane & 15, g = lane >> 4;
+  const bool wide = (((uintptr_t)a.q.ptr >> 1 | a.q.row_stride | a.q.head_stride) & 7u) == 0;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const uint32_t row = row0 + 16 * n + c16;
+    const bool in = row < x.n_rows;
+    const uint32_t tok = in ? row / a.group : 0u, hq = h * a.group + (in ? row % a.group : 0u);
+    pos[n] = in ? x.pos0 + (int)tok : -1;
+    const uint16_t *qp = (const uint16_t *)a.q.ptr + (uint64_t)(x.q0 + tok) * a.q.row_stride +
+                         (uint64_t)hq * a.q.head_stride + g * 16;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      const uint16_t *p = qp + (c >> 1) * 64 + (c & 1) * 8;
+      u32x4 e;
+      if (wide) {
+        e = *(const u32x4 *)p;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = (uint32_t)p[2 * j] | (uint32_t)p[2 * j + 1] << 16;
+      }
+      q[n][c] = __builtin_bit_cast(frag, e);
+    }
+  }
+}
+
+// A wave's rows into the output, or into the workspace if the tile has several
+// parts.  place: the workspace's place of row0.
+template <int DT, int FMT, int D, int NQ>
+__device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x, uint32_t row0,
+                                           uint32_t h, const Rows<D, NQ> &w, float lift,
+                                           bool whole, uint64_t place) {
+  const int lane = lane_id(), c16 = lane & 15, g = lane >> 4;
+  const bool wide = (((uintptr_t)a.out.ptr >> 1 | a.out.row_stride | a.out.head_stride) & 3u) == 0;
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const uint32_t row = row0 + 16 * n + c16;
+    if (row >= x.n_rows) continue;
+    const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? w.vref / w.l[n] : 0.0f;
+    const float lse2 = w.l[n] == 0.0f ? kNegInf : w.m[n] + __builtin_amdgcn_logf(w.l[n]) - lift;
+    if (!whole) {
+      const uint64_t to = place + 16 * n + c16;
+      float *po = a.part_out + to * D + 4 * g;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) *(f32x4 *)(po + 16 * j) = w.o[n][j] * inv;
+      if (g == 0) a.part_lse[to] = lse2;
+      continue;
+    }
+    const uint32_t tok = row / a.group, hq = h * a.group + row % a.group;
+    uint16_t *op = (uint16_t *)a.out.ptr + (uint64_t)(x.q0 + tok) * a.out.row_stride +
+                   (uint64_t)hq * a.out.head_stride + 4 * g;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const uint32_t u = Qk<DT, FMT>::two(w.o[n][j][0] * inv, w.o[n][j][1] * inv);
+      const uint32_t v = Qk<DT, FMT>::two(w.o[n][j][2] * inv, w.o[n][j][3] * inv);
+      if (wide) {
+        *(u32x2 *)(op + 16 * j) = u32x2{u, v};
+      } else {
+        op[16 * j] = (uint16_t)u;
+        op[16 * j + 1] = (uint16_t)(u >> 16);
+        op[16 * j + 2] = (uint16_t)v;
+        op[16 * j + 3] = (uint16_t)(v >> 16);
+      }
+    }
+    if (g == 0 && a.lse)
+      a.lse[(uint64_t)(x.q0 + tok) * (a.group * a.c.n_heads) + hq] = lse2 * 0.6931471805599453f;
+  }
+}
+
+// The work items of a call: a part of a tile of a request, for one key head.
+// They are counted on the device, by a scan over the requests' lengths that
+// every workgroup makes for itself, 256 requests at a time: lengths as
+// different as 1 and 100,000 in one call leave no workgroup without work.
+struct Items {
+  uint64_t pre[kAttThreads + 1], sums[kAttThreads / 64];
+  Request req[kAttThreads];
+};
+
+struct Item {
+  uint32_t r, h, tile, part;
+  Request x;
+};
+
+struct ItemWalk {
+  uint64_t base = 0;  // items before the requests that are in LDS
+  uint32_t r0 = 0;
+
+  __device__ __forceinline__ void scan(const AttendArgs &a, Items *s) {
+    const int wave = threadIdx.x >> 6, lane = lane_id();
+    const uint32_t r = r0 + threadIdx.x;
+    const bool mine = threadIdx.x < kAttThreads;  // a workgroup may have more threads
+    Request x = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (mine && r < a.n_requests) x = request_of(a, r, blockIdx.x == 0);
+    uint64_t n = (uint64_t)x.tiles * x.parts;
+    for (int i = 1; i < 64; i <<= 1) {
+      const uint64_t y = __shfl_up(n, i);
+      if (lane >= i) n += y;
+    }
+    __syncthreads();  // the readers of the requests before are done
+    if (mine && lane == 63) s->sums[wave] = n;
+    __syncthreads();
+    if (mine) {
+      for (int i = 0; i < wave; ++i) n += s->sums[i];
+      s->pre[threadIdx.x + 1] = n;
+      if (threadIdx.x == 0) s->pre[0] = 0;
+      s->req[threadIdx.x] = x;
+    }
+    __syncthreads();
+  }
+
+  // Item `at` (ascending from call to call); false behind the last one.  A
+  // request's last tiles come first: later rows see more.
+  __device__ __forceinline__ bool find(const AttendArgs &a, Items *s, uint64_t at, Item *it) {
+    const uint64_t item = at / a.c.n_heads;
+    it->h = (uint32_t)(at - item * a.c.n_heads);
+    while (item - base >= s->pre[kAttThreads]) {
+      base += s->pre[kAttThreads];
+      r0 += kAttThreads;
+      if (r0 >= a.n_requests) return false;
+      scan(a, s);
+    }
+    uint32_t i = 0;
+#pragma unroll
+    for (int k = kAttThreads / 2; k; k >>= 1)
+      if (s->pre[i + k] <= item - base) i += k;
+    i = __builtin_amdgcn_readfirstlane(i);
+    it->r = r0 + i;
+    it->x = uniform(s->req[i]);
+    const uint32_t k = __builtin_amdgcn_readfirstlane((uint32_t)(item - base - s->pre[i]));
+    it->tile = it->x.tiles - 1 - k / it->x.parts;
+    it->part = it->x.part0 + k % it->x.parts;
+    return true;
+  }
+};
+
+// The values of steps [first, last] that are not finite, for the rows that see
+// them (adding one twice changes nothing).  A cache of finite values never
+// gets here.
+template <int FMT, int D, int NQ>
+__device__ __forceinline__ void add_special(const AttendArgs &a, const Tile &t, uint32_t h,
+                                            const int32_t *row, uint32_t first, uint32_t last,
+                                            const int (&pos)[NQ], const int (&low)[NQ],
+                                            Rows<D, NQ> *w) {
+  const uint32_t bt = 1u << a.bt_log2;
+  const int g = lane_id() >> 4;
+  uint32_t j = first << 6, end = (last + 1) << 6;
+  j = j < t.lo ? t.lo : j;
+  end = end < t.hi ? end : t.hi;
+#pragma unroll 1
+  for (; j < end; ++j) {
+    const int32_t id = row[j >> a.bt_log2];
+    if ((uint32_t)id >= a.c.n_blocks) continue;
+    const uint8_t *v = (const uint8_t *)a.c.v + (uint64_t)id * a.c.v_stride +
+                       ((uint64_t)h * D + 4 * g) * bt + (j & (bt - 1));
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t b = v[(uint64_t)(16 * i + k) * bt];
+        const float y = Code<FMT>::special(b) & 0x80u ? Code<FMT>::value(b) : 0.0f;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+          w->o[n][i][k] += (int)j <= pos[n] && (int)j > low[n] ? y : 0.0f;
+      }
+  }
+}
+
 // Attention over a range of 64-token steps.  The scores are computed
 // transposed, S^T = K Q^T, with key row 4 a + b of tile t being token 16 a +
 // 4 t + b of the step: the result then leaves lane group a the weights of the
@@ -38,36 +235,9 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
   constexpr int KC = D / 64, VT = D / 16;
   const int lane = lane_id(), c16 = lane & 15, g = lane >> 4, ka = c16 >> 2, kb = c16 & 3;
   const uint32_t bt = 1u << a.bt_log2;
-  // queries: right operand, column = row of the tile, the same order of the
-  // head's dimensions as the keys' loads give
   frag q[NQ][2 * KC];
   int pos[NQ];
-  const bool wide = (((uintptr_t)a.q.ptr >> 1 | a.q.row_stride | a.q.head_stride) & 7u) == 0;
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const uint32_t row = t.row0 + 16 * n + c16;
-    const bool in = row < x.n_rows;
-    const uint32_t tok = in ? row / a.group : 0u, hq = h * a.group + (in ? row % a.group : 0u);
-    pos[n] = in ? x.pos0 + (int)tok : -1;
-    const uint16_t *qp = (const uint16_t *)a.q.ptr + (uint64_t)(x.q0 + tok) * a.q.row_stride +
-                         (uint64_t)hq * a.q.head_stride + g * 16;
-    if (wide) {
-#pragma unroll
-      for (int c = 0; c < 2 * KC; ++c)
-        q[n][c] = __builtin_bit_cast(frag, *(const u32x4 *)(qp + (c >> 1) * 64 + (c & 1) * 8));
-    } else {
-#pragma unroll
-      for (int c = 0; c < 2 * KC; ++c) {
-        u32x4 e;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint16_t *p = qp + (c >> 1) * 64 + (c & 1) * 8 + 2 * j;
-          e[j] = (uint32_t)p[0] | (uint32_t)p[1] << 16;
-        }
-        q[n][c] = __builtin_bit_cast(frag, e);
-      }
-    }
-  }
+  load_queries<DT, FMT, D, NQ>(a, x, t.row0, h, q, pos);
   // the lane's part of a block's keys and values
   const uint8_t *kbase = (const uint8_t *)a.c.k + ((uint64_t)h * bt + kb) * D + g * 16;
   const uint8_t *vbase = (const uint8_t *)a.c.v + ((uint64_t)h * D + c16) * bt;
@@ -122,6 +292,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
     load_keys(idk, step0 << 6);
     load_values(idv, step0 << 6);
   }
+  uint32_t sp_first = ~0u, sp_last = 0;  // steps with values that were taken out
   for (uint32_t s = step0; s < step1; s += 4) {
     const uint32_t t0 = s << 6;
     const bool more = s + 4 < step1;
@@ -170,9 +341,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
       }
     }
     // the values' unit: the largest scale so far
-    float vmax = fabsf(vs);
-    vmax = fmaxf(vmax, __shfl_xor(vmax, 16));
-    vmax = fmaxf(vmax, __shfl_xor(vmax, 32));
+    const float vmax = group_max(fabsf(vs));
     const float vref = fmaxf(w->vref, vmax);
     const float vscale = vs / vref, shrink = w->vref / vref;
     w->vref = vref;
@@ -184,8 +353,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[n][i][j]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
+      top = group_max(top);
       const float use = top == kNegInf ? 0.0f : top;  // nothing seen yet: every weight is 0
       const float keep = __builtin_amdgcn_exp2f(w->m[n] - use);
       w->m[n] = top;
@@ -220,59 +388,31 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
       return o;
     };
     // values that are not finite and that some row does not see: a weight of
-    // 0 would not keep them out of the product
-    bool special = false;
+    // 0 would not keep them out of the product.  They are taken out here, and
+    // the rows that see them get them at the end.
     if (masked) {
       uint32_t any = 0;
 #pragma unroll
       for (int i = 0; i < VT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) any |= Code<FMT>::special(vr[i][j]);
-      special = __any((any & 0x80808080u) != 0);
+        for (int j = 0; j < 4; ++j) any |= take_special<FMT>(vr[i], j);
+      if (__any(any != 0)) {
+        sp_first = s < sp_first ? s : sp_first;
+        sp_last = s;
+      }
     }
-    if (special) {
-      // a row at a time, with only the codes that it sees (a loop that a cache
-      // of finite values never enters); a weight below half precision counts
-      // as its smallest, so that an infinity stays one
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
+    for (int i = 0; i < VT; ++i)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (sc[n][i >> 2][i & 3] > kNegInf && p[n][i >> 3][i & 7] == (_Float16)0.0f)
-            p[n][i >> 3][i & 7] = (_Float16)copysignf(0x1p-24f, vscale);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll 1
-        for (int c = 0; c < 16; ++c) {
-          // the places that row c sees (every lane asks lane c)
-          const int last = __shfl(pos[n], c) - first, begin = __shfl(low[n], c) - first;
-          const int end = idv < 0 ? -1 : last;
-          u32x4 m;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            m[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (4 * i + j <= end && 4 * i + j > begin) m[i] |= 0xFFu << (8 * j);
-          }
-#pragma unroll
-          for (int i = 0; i < VT; ++i) {
-            const f32x4 o = accumulate(n, i, vr[i] & m);
-            if (c16 == c) w->o[n][i] = o;
-          }
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VT; ++i)
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) w->o[n][i] = accumulate(n, i, vr[i]);
-    }
+      for (int n = 0; n < NQ; ++n) w->o[n][i] = accumulate(n, i, vr[i]);
     if (kAhead && more) {
       idv = idv1;
       load_values(idv, t0 + 256);
       blocks(s + 8);
     }
   }
+  if (sp_first <= sp_last)
+    add_special<FMT, D, NQ>(a, t, h, row, sp_first, sp_last, pos, low, w);
   // a lane has summed its own tokens: the rows' sums over the lane groups
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -328,75 +468,28 @@ constexpr int resident(int d, int nq) {
   return d * nq <= 64 ? 3 : 2;
 }
 
-// The grid is as large as the GPU holds; its workgroups take the work items
-// (a part of a tile of a request, for one key head) in turn.  The items are counted on the
-// device, by a scan over the requests' lengths that every workgroup makes
-// for itself, 256 requests at a time: lengths as different as 1 and 100,000
-// in one call leave no workgroup without work and none with a long rest.
+// Few rows: the grid is as large as the GPU holds, its workgroups take the
+// items in turn.
 template <int DT, int FMT, int D, int NQ>
 __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendArgs a) {
   __shared__ Parked<D, NQ> parked[2];
-  __shared__ uint64_t pre[kAttThreads + 1], sums[kAttThreads / 64];
-  __shared__ Request req[kAttThreads];
+  __shared__ Items items;
   const int wave = threadIdx.x >> 6, lane = lane_id();
-  const uint32_t heads = a.c.n_heads;
-  uint64_t base = 0;  // items before the requests in pre
-  uint32_t r0 = 0;
-  auto scan = [&]() {
-    const uint32_t r = r0 + threadIdx.x;
-    Request x = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (r < a.n_requests) x = request_of(a, r, blockIdx.x == 0);
-    uint64_t n = (uint64_t)x.tiles * x.parts;
-    for (int i = 1; i < 64; i <<= 1) {
-      const uint64_t y = __shfl_up(n, i);
-      if (lane >= i) n += y;
-    }
-    __syncthreads();  // pre's readers are done
-    if (lane == 63) sums[wave] = n;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) n += sums[i];
-    pre[threadIdx.x + 1] = n;
-    if (threadIdx.x == 0) pre[0] = 0;
-    req[threadIdx.x] = x;
-    __syncthreads();
-  };
-  scan();
-  for (uint64_t at = blockIdx.x;; at += gridDim.x) {
-    const uint64_t item = at / heads;
-    const uint32_t h = (uint32_t)(at - item * heads);
-    while (item - base >= pre[kAttThreads]) {
-      base += pre[kAttThreads];
-      r0 += kAttThreads;
-      if (r0 >= a.n_requests) return;
-      scan();
-    }
-    uint32_t i = 0;
-#pragma unroll
-    for (int k = kAttThreads / 2; k; k >>= 1)
-      if (pre[i + k] <= item - base) i += k;
-    i = __builtin_amdgcn_readfirstlane(i);
-    const uint32_t r = r0 + i;
-    const Request x = uniform(req[i]);
-    const uint32_t k = (uint32_t)(item - base - pre[i]);
-    const uint32_t tile = __builtin_amdgcn_readfirstlane(k / x.parts);
-    const uint32_t part = __builtin_amdgcn_readfirstlane(x.part0 + k % x.parts);
-    const Tile t = tile_of(a, x, tile);
+  ItemWalk walk;
+  walk.scan(a, &items);
+  Item it;
+  for (uint64_t at = blockIdx.x; walk.find(a, &items, at, &it); at += gridDim.x) {
+    const Request &x = it.x;
+    const Tile t = tile_of(a, x, it.tile);
     const bool none = t.part0 == t.part1;  // no row sees anything: the first item says so
-    if (none ? part != x.part0 : (part < t.part0 || part >= t.part1)) continue;
+    if (none ? it.part != x.part0 : (it.part < t.part0 || it.part >= t.part1)) continue;
     Rows<D, NQ> w;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      w.m[n] = kNegInf;
-      w.l[n] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) w.o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    w.vref = 0x1p-125f;  // below it a scale has no exact reciprocal
+    clear(&w);
     // steps of the part, wave w those that are w modulo 4
-    uint32_t s0 = part << (x.cut - 6), s1 = (uint32_t)(((uint64_t)t.hi + 63) >> 6);
+    uint32_t s0 = it.part << (x.cut - 6), s1 = (uint32_t)(((uint64_t)t.hi + 63) >> 6);
     if (s1 > s0 + (1u << (x.cut - 6))) s1 = s0 + (1u << (x.cut - 6));
     if (s0 < t.lo >> 6) s0 += ((t.lo >> 6) - s0) & ~3u;
-    if (!none) attend_steps<DT, FMT, D, NQ>(a, r, x, t, h, s0 + wave, s1, &w);
+    if (!none) attend_steps<DT, FMT, D, NQ>(a, it.r, x, t, it.h, s0 + wave, s1, &w);
     __syncthreads();  // wave 0 has read the item before's
     if (wave >= 2) park(w, &parked[wave - 2], lane);
     __syncthreads();
@@ -406,49 +499,339 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
     __syncthreads();
     if (wave) continue;
     join(&w, parked[0], lane);
-    const int c16 = lane & 15, g = lane >> 4;
-    const uint32_t n_parts = t.part1 - t.part0;
+    const bool whole = t.part1 - t.part0 <= 1;
+    store_rows<DT, FMT, D, NQ>(
+        a, x, t.row0, it.h, w, kLift, whole,
+        whole ? 0 : part_place(a, x, it.r, it.tile, it.part - t.part0, it.h));
+  }
+}
+
+// ---- many rows --------------------------------------------------------------
+//
+// Prompts: a tile of 128 rows, 16 NQ of them per wave, and every wave goes
+// through all of the tile's steps.  A step's keys and values are converted
+// once for all waves, each a share, and lie in LDS as the matrix instructions' left operands, 16 bytes
+// a lane in lane order: reads and writes without bank conflicts.  Two steps'
+// worth, so one barrier a step.
+//
+// What bounds it is the vector ALU beside the matrix cores (half a maximum, an
+// exponential, two fused products and a rounding per score), so little else
+// is done per score: scores are scaled within the exponent's product, which
+// also takes the values' scale (the sum of the weights takes it out again), a
+// row's maximum moves only when it has grown 2^4 fold (weights are at most
+// 2^15 all the same: the lift is 4 less), and steps that every row sees whole
+// run in a loop without masks.
+constexpr float kSlack = 4.0f, kLiftMany = 11.0f;
+
+// Row blocks of a wave.  Two leave room for a second wave on the SIMD, whose
+// products run beside this one's exponentials (three or four blocks read LDS
+// less often, but were slower: 288 and 524 us where two take 256).
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
+
+//
+// 192 dimensions and more: twice the waves with a block each, so that the sums
+// still fit into 256 registers; the tile is 128 rows either way.
+constexpr int many_waves(int d) { return d <= 128 ? 4 : 8; }
+
+template <int DT, int FMT, int D>
+__global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArgs a) {
+  typedef Qk<DT, FMT> T;
+  typedef Qk<WM_FP16, FMT> V;
+  typedef typename T::frag frag;
+  constexpr int kWaves = many_waves(D), NQ = 8 / kWaves, KC = D / 64, VT = D / 16;
+  // a wave's share of a step: of key tile wave % 4 every KS-th 64 dimensions,
+  // and every kWaves-th value tile
+  constexpr int KS = kWaves / 4, KW = (KC + KS - 1) / KS, VW = (VT + kWaves - 1) / kWaves;
+  __shared__ u32x4 kf[2][8 * KC][64];  // [step][4 tiles x 2 KC][lane]
+  __shared__ u32x4 vf[2][2 * VT][64];
+  __shared__ uint32_t special[2][kWaves];
+  __shared__ Items items;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
+  const int c16 = lane & 15, g = lane >> 4, ka = c16 >> 2, kb = c16 & 3;
+  const uint32_t bt = 1u << a.bt_log2;
+  ItemWalk walk;
+  walk.scan(a, &items);
+  Item it;
+  if (!walk.find(a, &items, blockIdx.x, &it)) return;
+  const Request &x = it.x;
+  const Tile t = tile_of(a, x, it.tile);
+  const bool none = t.part0 == t.part1;
+  if (none ? it.part != x.part0 : (it.part < t.part0 || it.part >= t.part1)) return;
+  const uint32_t h = it.h, row0 = t.row0 + wave * 16 * NQ;
+  frag q[NQ][2 * KC];
+  int pos[NQ], low[NQ];
+  load_queries<DT, FMT, D, NQ>(a, x, row0, h, q, pos);
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      const uint32_t row = t.row0 + 16 * n + c16;
-      if (row >= x.n_rows) continue;
-      const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? w.vref / w.l[n] : 0.0f;
-      const float lse2 = w.l[n] == 0.0f ? kNegInf : w.m[n] + __builtin_amdgcn_logf(w.l[n]) - kLift;
-      if (n_parts > 1) {
-        const uint64_t to = part_place(a, x, r, tile, part - t.part0, h) + 16 * n + c16;
-        float *po = a.part_out + to * D + 4 * g;
+  for (int n = 0; n < NQ; ++n) low[n] = a.window ? pos[n] - (int)a.window : -1;
+  // a negative factor of the scores goes into the queries
+  const float scale = fabsf(a.scale_log2);
+  if (a.scale_log2 < 0.0f) {
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) *(f32x4 *)(po + 16 * j) = w.o[n][j] * inv;
-        if (g == 0) a.part_lse[to] = lse2;
-      } else {
-        const uint32_t tok = row / a.group, hq = h * a.group + row % a.group;
-        uint16_t *op = (uint16_t *)a.out.ptr + (uint64_t)(x.q0 + tok) * a.out.row_stride +
-                       (uint64_t)hq * a.out.head_stride + 4 * g;
-        const bool wide =
-            (((uintptr_t)a.out.ptr >> 1 | a.out.row_stride | a.out.head_stride) & 3u) == 0;
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-          const uint32_t u = Qk<DT, FMT>::two(w.o[n][j][0] * inv, w.o[n][j][1] * inv);
-          const uint32_t v = Qk<DT, FMT>::two(w.o[n][j][2] * inv, w.o[n][j][3] * inv);
-          if (wide) {
-            *(u32x2 *)(op + 16 * j) = u32x2{u, v};
-          } else {
-            op[16 * j] = (uint16_t)u;
-            op[16 * j + 1] = (uint16_t)(u >> 16);
-            op[16 * j + 2] = (uint16_t)v;
-            op[16 * j + 3] = (uint16_t)(v >> 16);
-          }
-        }
-        if (g == 0 && a.lse)
-          a.lse[(uint64_t)(x.q0 + tok) * (a.group * heads) + hq] = lse2 * 0.6931471805599453f;
+      for (int c = 0; c < 2 * KC; ++c)
+        q[n][c] = __builtin_bit_cast(frag, __builtin_bit_cast(u32x4, q[n][c]) ^ 0x80008000u);
+  }
+  // tokens [w_lo, w_hi) are seen by some row of the wave (rows behind the
+  // request's last are not stored: what they see does not matter)
+  const uint32_t row1 = row0 + 16 * NQ - 1 < x.n_rows ? row0 + 16 * NQ - 1 : x.n_rows - 1;
+  const int p_first = x.pos0 + (int)(row0 / a.group), p_last = x.pos0 + (int)(row1 / a.group);
+  const bool idle = row0 >= x.n_rows;
+  const int w_hi = idle ? 0 : p_last + 1;
+  const int w_lo = a.window && p_first + 1 > (int)a.window ? p_first + 1 - (int)a.window : 0;
+  Rows<D, NQ> w;
+  clear(&w);
+  float vref = w.vref;  // the tile's; w.vref is the one of the wave's last step
+  const uint32_t s_part = it.part << (x.cut - 6);
+  uint32_t s0 = t.lo >> 6, s1 = none ? 0u : (uint32_t)(((uint64_t)t.hi + 63) >> 6);
+  if (s0 < s_part) s0 = s_part;
+  if (s1 > s_part + (1u << (x.cut - 6))) s1 = s_part + (1u << (x.cut - 6));
+
+  const uint8_t *kbase = (const uint8_t *)a.c.k + ((uint64_t)h * bt + kb + 4 * (wave & 3)) * D +
+                         (wave >> 2) * 64 + g * 16;
+  const uint8_t *vbase = (const uint8_t *)a.c.v + ((uint64_t)h * D + 16 * wave + c16) * bt;
+  const int32_t *row = a.table + (uint64_t)it.r * a.table_stride;
+  bool bad_page = false;
+  auto block_of = [&](uint32_t j) -> int32_t {
+    const bool in = j < t.hi && j + 16 > t.lo;
+    const int32_t id = row[(in ? j : t.lo) >> a.bt_log2];
+    const bool out = in && (uint32_t)id >= a.c.n_blocks;
+    bad_page |= out;
+    return in && !out ? id : -1;
+  };
+  // does the wave have share j of the keys, of the values?
+  auto has_k = [&](int j) { return KC % KS == 0 || (wave >> 2) + KS * j < KC; };
+  auto has_v = [&](int j) { return VT % kWaves == 0 || wave + kWaves * j < VT; };
+  u32x4 kg[KW], vg[VW];
+  float ks1 = 0.0f, vs1 = 0.0f;
+  int32_t idk1 = -1, idv1 = -1, idk2 = -1, idv2 = -1;  // of the step that is loaded, and of the one after
+  auto blocks = [&](uint32_t s) {
+    idk2 = block_of((s << 6) + 16 * ka);
+    idv2 = block_of((s << 6) + 16 * g);
+  };
+  auto load = [&](uint32_t s) {
+    const uint32_t t0 = s << 6;
+    const uint8_t *kp = kbase + (uint64_t)(idk2 < 0 ? 0 : idk2) * a.c.k_stride +
+                        ((t0 + 16 * ka) & (bt - 1)) * D;
+    const uint8_t *vp = vbase + (uint64_t)(idv2 < 0 ? 0 : idv2) * a.c.v_stride +
+                        ((t0 + 16 * g) & (bt - 1));
+    idk1 = idk2;
+    idv1 = idv2;
+#pragma unroll
+    for (int j = 0; j < KW; ++j)
+      if (has_k(j)) kg[j] = *(const u32x4 *)(kp + j * KS * 64);
+#pragma unroll
+    for (int j = 0; j < VW; ++j)
+      if (has_v(j)) vg[j] = *(const u32x4 *)(vp + (uint64_t)j * kWaves * 16 * bt);
+    ks1 = a.c.k_scale[(uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.k_scale_stride + h];
+    vs1 = a.c.v_scale[(uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_scale_stride + h];
+  };
+  if (s0 < s1) {
+    blocks(s0);
+    load(s0);
+    blocks(s0 + 1);
+  }
+  uint32_t sp_first = ~0u, sp_last = 0;  // steps with values that were taken out
+  auto step = [&](uint32_t s, auto mask_tag) {
+    constexpr bool kMasked = decltype(mask_tag)::value;
+    const int b = s & 1;
+    const int32_t idv = idv1;
+    // a block that is not there: no codes that could be NaN, scales of 0
+    const float ks = idv < 0 ? 0.0f : ks1, vs = idv < 0 ? 0.0f : vs1;
+    const uint32_t k_there = idk1 < 0 ? 0u : ~0u, v_there = idv < 0 ? 0u : ~0u;
+    uint32_t sp = 0;
+#pragma unroll
+    for (int j = 0; j < KW; ++j)
+      if (has_k(j)) {
+        kg[j] &= k_there;
+        const int at = (wave & 3) * 2 * KC + 2 * ((wave >> 2) + KS * j);
+        kf[b][at][lane] = __builtin_bit_cast(u32x4, T::key(kg[j][0], kg[j][1]));
+        kf[b][at + 1][lane] = __builtin_bit_cast(u32x4, T::key(kg[j][2], kg[j][3]));
+      }
+#pragma unroll
+    for (int j = 0; j < VW; ++j)
+      if (has_v(j)) {
+        vg[j] &= v_there;
+        if (kMasked)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sp |= take_special<FMT>(vg[j], k);
+        const int at = 2 * (wave + kWaves * j);
+        vf[b][at][lane] = __builtin_bit_cast(u32x4, V::key(vg[j][0], vg[j][1]));
+        vf[b][at + 1][lane] = __builtin_bit_cast(u32x4, V::key(vg[j][2], vg[j][3]));
+      }
+    if (kMasked) {
+      sp = __any(sp != 0);
+      if (lane == 0) special[b][wave] = sp;
+    }
+    if (s + 1 < s1) {
+      load(s + 1);
+      blocks(s + 2);
+    }
+    // the values' unit is the largest scale so far
+    vref = fmaxf(vref, group_max(vs));
+    const float ratio = fmaxf(vs / vref, 0x1p-60f);
+    __syncthreads();
+    const int t0 = (int)(s << 6);
+    if (kMasked) {
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) any |= special[b][i];
+      if (__builtin_amdgcn_readfirstlane(any)) {
+        sp_first = s < sp_first ? s : sp_first;
+        sp_last = s;
       }
     }
+    if (kMasked && (t0 >= w_hi || t0 + 63 < w_lo)) return;  // nothing for this wave
+    f32x4 sc[NQ][4];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[n][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // LDS is read four operands ahead of the products: the barriers keep the
+    // compiler from putting a read right before its use
+    u32x4 ahead[2][4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) ahead[0][c] = kf[b][c][lane];
+#pragma unroll
+    for (int j = 0; j < 2 * KC; ++j) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        ahead[(j + 1) & 1][c] = j + 1 < 2 * KC ? kf[b][4 * (j + 1) + c][lane] : vf[b][c][lane];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int i = (4 * j + c) / (2 * KC), d = (4 * j + c) % (2 * KC);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+          sc[n][i] = T::mma(__builtin_bit_cast(frag, ahead[j & 1][c]), q[n][d], sc[n][i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float cs = ks * scale;  // not negative: a row's largest score is its largest sum
+    const int first = t0 + 16 * g;
+    if (kMasked) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const int end = idv < 0 ? -1 : pos[n] - first, begin = low[n] - first;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float y = sc[n][i >> 2][i & 3] * cs;
+          sc[n][i >> 2][i & 3] = i > end || i <= begin ? kNegInf : y;
+        }
+      }
+    }
+    const float f = kMasked ? 1.0f : cs;
+    float top[NQ];
+    bool grows = w.vref != vref;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float y = sc[n][0][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) y = fmaxf(y, sc[n][i >> 2][i & 3]);
+      y *= f;
+      top[n] = group_max(!kMasked && idv < 0 ? kNegInf : y);
+      grows |= top[n] > w.m[n] + kSlack;
+    }
+    if (__any(grows)) {
+      const float shrink = w.vref / vref;
+      w.vref = vref;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float m = fmaxf(w.m[n], top[n]);
+        const float keep = __builtin_amdgcn_exp2f(w.m[n] - (m == kNegInf ? 0.0f : m));
+        w.m[n] = m;
+        w.l[n] *= keep;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) w.o[n][i] *= keep * shrink;
+      }
+    }
+    const float back = 1.0f / ratio, lift = kLiftMany + __builtin_amdgcn_logf(ratio);
+    f16x8 p[NQ][2], p_low[NQ][2];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      float add = lift - (w.m[n] == kNegInf ? 0.0f : w.m[n]);
+      if (!kMasked) add = idv < 0 ? kNegInf : add;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i >> 2][i & 3], f, add));
+        w.l[n] = __builtin_fmaf(y, back, w.l[n]);
+        const _Float16 hi = (_Float16)y;
+        p[n][i >> 3][i & 7] = hi;
+        if (DT == WM_FP16) p_low[n][i >> 3][i & 7] = (_Float16)(y - (float)hi);
+      }
+    }
+    auto accumulate = [&](int n, f32x4 o, f16x8 v0, f16x8 v1) -> f32x4 {
+      o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][0], o, 0, 0, 0);
+      o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[n][1], o, 0, 0, 0);
+      if (DT == WM_FP16) {
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p_low[n][0], o, 0, 0, 0);
+        o = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p_low[n][1], o, 0, 0, 0);
+      }
+      return o;
+    };
+#pragma unroll
+    for (int i = 0; i < VT / 2; ++i) {
+      if (i + 1 < VT / 2) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) ahead[(i + 1) & 1][c] = vf[b][4 * (i + 1) + c][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+          w.o[n][2 * i + k] = accumulate(n, w.o[n][2 * i + k],
+                                         __builtin_bit_cast(f16x8, ahead[i & 1][2 * k]),
+                                         __builtin_bit_cast(f16x8, ahead[i & 1][2 * k + 1]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // steps [s_a, s_b) are seen whole by every row of the tile
+  uint32_t s_a = s0, s_b = s1;
+  {
+    const uint32_t last = t.row0 + 127 < x.n_rows ? t.row0 + 127 : x.n_rows - 1;
+    const int t_first = x.pos0 + (int)(t.row0 / a.group), t_last = x.pos0 + (int)(last / a.group);
+    const uint32_t whole = t_first < 0 ? 0u : (uint32_t)(t_first + 1) >> 6;
+    if (a.window && t_last + 1 > (int)a.window)
+      s_a = (uint32_t)(t_last + 1 - (int)a.window + 63) >> 6;
+    s_a = s_a < s0 ? s0 : (s_a > s1 ? s1 : s_a);
+    s_b = whole < s_a ? s_a : (whole > s1 ? s1 : whole);
   }
+  for (uint32_t s = s0; s < s1;) {
+    const bool masked = s < s_a || s >= s_b;
+    const uint32_t end = s < s_a ? s_a : (s < s_b ? s_b : s1);
+    if (masked)
+      for (; s < end; ++s) step(s, Yes{});
+    else
+      for (; s < end; ++s) step(s, No{});
+  }
+  if (sp_first <= sp_last)
+    add_special<FMT, D, NQ>(a, t, h, row, sp_first, sp_last, pos, low, &w);
+  if (__any(bad_page) && lane == 0 && a.verdict) atomicOr(a.verdict, WM_C_PAGE);
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    w.l[n] += __shfl_xor(w.l[n], 16);
+    w.l[n] += __shfl_xor(w.l[n], 32);
+  }
+  if (idle) return;
+  const bool whole = t.part1 - t.part0 <= 1;
+  store_rows<DT, FMT, D, NQ>(
+      a, x, row0, h, w, kLiftMany, whole,
+      whole ? 0 : part_place(a, x, it.r, it.tile, it.part - t.part0, h) + wave * 16 * NQ);
 }
 
 template <int DT, int FMT, int D>
 int attend_rows(const AttendArgs &a, hipStream_t st) {
   const uint64_t most = (uint64_t)a.plan.tiles * a.c.n_heads * a.plan.splits;
+  if (a.plan.rows > 32) {
+    k_attend_many<DT, FMT, D><<<(uint32_t)most, 64 * many_waves(D), 0, st>>>(a);
+    return (int)hipGetLastError();
+  }
   const uint64_t room = (uint64_t)a.n_cu * resident(D, a.plan.rows / 16);
   const uint32_t grid = (uint32_t)(most < room ? most : room);
   if (a.plan.rows == 16)

@@ -120,14 +120,23 @@ namespace wm {
 
 AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
                        uint32_t n_q_heads, uint32_t head_dim, uint32_t max_len) {
-  AttendPlan p = {16, 1, 1};
+  AttendPlan p = {16, 1, 1, 9};
   if (!n_requests || !n_tokens || !n_heads || n_q_heads < n_heads) return p;
-  const uint64_t rows = (uint64_t)n_tokens * (n_q_heads / n_heads);
-  (void)head_dim;
-  if (rows > 16ull * n_requests) p.rows = 32;
+  const uint64_t rows = (uint64_t)n_tokens * (n_q_heads / n_heads), each = rows / n_requests;
+  const uint64_t len = std::max<uint64_t>(1, max_len);
+  if (each > 32)
+    p.rows = 128;
+  else if (each > 16)
+    p.rows = 32;
   p.tiles = (uint32_t)(rows / p.rows + n_requests);
+  if (p.rows > 32) {
+    // a sequence is cut only where its tiles leave more than half of 256 CUs idle
+    const uint64_t busy = std::max<uint64_t>(rows / p.rows, n_requests) * n_heads;
+    const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>(256 / busy, 31));
+    while (((len - 1) >> p.cut) + 1 > want) ++p.cut;
+  }
   // parts of 512 tokens, or of more so that there are at most 32
-  p.splits = (uint32_t)std::min<uint64_t>(32, std::max<uint64_t>(1, (max_len + 511ull) / 512));
+  p.splits = (uint32_t)std::min<uint64_t>(32, ((len - 1) >> p.cut) + 1);
   return p;
 }
 

@@ -72,8 +72,8 @@ struct Code<WM_E4M3> {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI);
   }
   template <bool HI>
-  static __device__ __forceinline__ f16x2 half(uint32_t w) {
-    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI);
+  static __device__ __forceinline__ f16x2 half(uint32_t w, float pow2 = 1.0f) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, pow2, HI);
   }
 };
 template <>
@@ -93,10 +93,19 @@ struct Code<WM_E5M2> {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, HI);
   }
   template <bool HI>
-  static __device__ __forceinline__ f16x2 half(uint32_t w) {
-    return __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, 1.0f, HI);
+  static __device__ __forceinline__ f16x2 half(uint32_t w, float pow2 = 1.0f) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, pow2, HI);
   }
 };
+
+// Makes those of the four codes x[j] zero that have no finite value; nonzero
+// if there was one.
+template <int FMT>
+__device__ __forceinline__ uint32_t take_special(u32x4 &x, int j) {
+  const uint32_t sp = Code<FMT>::special(x[j]) & 0x80808080u;
+  x[j] &= ~((sp >> 7) * 0xFFu);
+  return sp;
+}
 
 template <int DT>
 __device__ __forceinline__ float load_elem(const void *p, uint64_t i) {
@@ -121,7 +130,7 @@ struct Request {
 };
 
 __device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, bool tell) {
-  Request x = {0, 0, 0, 0, 0, 9, 0, 1};
+  Request x = {0, 0, 0, 0, 0, a.plan.cut, 0, 1};
   int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1], len = a.len[r];
   q0 = q0 > 0 ? q0 : 0;
   q1 = q1 < (int64_t)a.n_tokens ? q1 : (int64_t)a.n_tokens;
@@ -217,6 +226,13 @@ struct Qk<WM_FP16, FMT> {
   static __device__ __forceinline__ frag key(uint32_t x, uint32_t y) {
     const f16x2 p = Code<FMT>::template half<false>(x), q = Code<FMT>::template half<true>(x);
     const f16x2 r = Code<FMT>::template half<false>(y), s = Code<FMT>::template half<true>(y);
+    return frag{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+  }
+  // eight values times a power of two
+  static __device__ __forceinline__ frag value(uint32_t x, uint32_t y, float pow2) {
+    typedef Code<FMT> C;
+    const f16x2 p = C::template half<false>(x, pow2), q = C::template half<true>(x, pow2);
+    const f16x2 r = C::template half<false>(y, pow2), s = C::template half<true>(y, pow2);
     return frag{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
   }
   static __device__ __forceinline__ f32x4 mma(frag k, frag q, f32x4 c) {

@@ -37,6 +37,7 @@ struct AttendPlan {
   uint32_t rows;    // query rows (tokens x group) of a tile
   uint32_t tiles;   // tile places: at least the tiles of every request
   uint32_t splits;  // most parts that a tile's sequence is cut into: 1..32
+  uint32_t cut;     // a part has 2^cut tokens at least
 };
 AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
                        uint32_t n_q_heads, uint32_t head_dim, uint32_t max_len);
