@@ -141,23 +141,20 @@ struct ItemWalk {
   __device__ __forceinline__ void scan(const AttendArgs &a, Items *s) {
     const int wave = threadIdx.x >> 6, lane = lane_id();
     const uint32_t r = r0 + threadIdx.x;
-    const bool mine = threadIdx.x < kAttThreads;  // a workgroup may have more threads
-    Request x = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (mine && r < a.n_requests) x = request_of(a, r, blockIdx.x == 0);
+    Request x = {};
+    if (r < a.n_requests) x = request_of(a, r, blockIdx.x == 0);
     uint64_t n = (uint64_t)x.tiles * x.parts;
     for (int i = 1; i < 64; i <<= 1) {
       const uint64_t y = __shfl_up(n, i);
       if (lane >= i) n += y;
     }
     __syncthreads();  // the readers of the requests before are done
-    if (mine && lane == 63) s->sums[wave] = n;
+    if (lane == 63) s->sums[wave] = n;
     __syncthreads();
-    if (mine) {
-      for (int i = 0; i < wave; ++i) n += s->sums[i];
-      s->pre[threadIdx.x + 1] = n;
-      if (threadIdx.x == 0) s->pre[0] = 0;
-      s->req[threadIdx.x] = x;
-    }
+    for (int i = 0; i < wave; ++i) n += s->sums[i];
+    s->pre[threadIdx.x + 1] = n;
+    if (threadIdx.x == 0) s->pre[0] = 0;
+    s->req[threadIdx.x] = x;
     __syncthreads();
   }
 
@@ -246,11 +243,12 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
 #pragma unroll
   for (int n = 0; n < NQ; ++n) low[n] = a.window ? pos[n] - (int)a.window : -1;
   bool bad_page = false;
-  // the block of token j (j a multiple of 16), -1 if no row sees its 16 tokens
-  auto block_of = [&](uint32_t j) -> int32_t {
-    const bool in = j < t.hi && j + 16 > t.lo;
-    const int32_t id = row[(in ? j : t.lo) >> a.bt_log2];  // lo < hi: an entry of the table
-    const bool out = in && (uint32_t)id >= a.c.n_blocks;
+  // the table's entry for token j (a multiple of 16), and the block that it is:
+  // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
+  // when it is needed: looking at once would wait for it.)
+  auto entry_of = [&](uint32_t j) { return row[(j < t.hi && j + 16 > t.lo ? j : t.lo) >> a.bt_log2]; };
+  auto block_of = [&](int32_t id, uint32_t j) -> int32_t {
+    const bool in = j < t.hi && j + 16 > t.lo, out = in && (uint32_t)id >= a.c.n_blocks;
     bad_page |= out;
     return in && !out ? id : -1;
   };
@@ -279,16 +277,20 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
     vs = a.c.v_scale[(uint64_t)(id < 0 ? 0 : id) * a.c.v_scale_stride + h];
     vs = id < 0 ? 0.0f : vs;
   };
-  int32_t idk = -1, idv = -1, idk1 = -1, idv1 = -1;  // this step's, and the next one's blocks
-  auto blocks = [&](uint32_t s) {
-    idk1 = block_of((s << 6) + 16 * ka);
-    idv1 = block_of((s << 6) + 16 * g);
+  int32_t idk = -1, idv = -1;  // the step's blocks
+  int32_t ek = 0, ev = 0;      // the next one's entries
+  auto entries = [&](uint32_t s) {
+    ek = entry_of((s << 6) + 16 * ka);
+    ev = entry_of((s << 6) + 16 * g);
   };
-  if (step0 < step1) blocks(step0);
+  auto blocks = [&](uint32_t s) {
+    idk = block_of(ek, (s << 6) + 16 * ka);
+    idv = block_of(ev, (s << 6) + 16 * g);
+  };
+  if (step0 < step1) entries(step0);
   if (kAhead && step0 < step1) {
-    idk = idk1;
-    idv = idv1;
-    blocks(step0 + 4);
+    blocks(step0);
+    entries(step0 + 4);
     load_keys(idk, step0 << 6);
     load_values(idv, step0 << 6);
   }
@@ -297,11 +299,10 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
     const uint32_t t0 = s << 6;
     const bool more = s + 4 < step1;
     if (!kAhead) {
-      idk = idk1;
-      idv = idv1;
+      blocks(s);
       load_keys(idk, t0);
       load_values(idv, t0);
-      blocks(s + 4);
+      entries(s + 4);
     }
     f32x4 sc[NQ][4];
 #pragma unroll
@@ -319,7 +320,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
           sc[n][i] = T::mma(k1, q[n][2 * c + 1], sc[n][i]);
         }
       }
-    if (kAhead && more) load_keys(idk1, t0 + 256);
+    if (kAhead && more) load_keys(block_of(ek, t0 + 256 + 16 * ka), t0 + 256);
     // masks: only where some row does not see some of the 64 tokens
     const float cs = ks * a.scale_log2;
     const int first = (int)(t0 + 16 * g);  // the lane's first token
@@ -406,9 +407,9 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
 #pragma unroll
       for (int n = 0; n < NQ; ++n) w->o[n][i] = accumulate(n, i, vr[i]);
     if (kAhead && more) {
-      idv = idv1;
+      idv = block_of(ev, t0 + 256 + 16 * g);
       load_values(idv, t0 + 256);
-      blocks(s + 8);
+      entries(s + 8);
     }
   }
   if (sp_first <= sp_last)
@@ -526,6 +527,59 @@ constexpr float kSlack = 4.0f, kLiftMany = 11.0f;
 // Row blocks of a wave.  Two leave room for a second wave on the SIMD, whose
 // products run beside this one's exponentials (three or four blocks read LDS
 // less often, but were slower: 288 and 524 us where two take 256).
+// (Written out: fmaxf would first turn each operand's signalling NaN quiet.)
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+  return r;
+}
+
+// The item of a workgroup: part and tile (a request's last tiles, which see
+// most, first) of a request, and a head.  A wave counts the items 64 requests
+// at a time, so that the workgroups with work are side by side and spread
+// evenly over the CUs; above 512 requests that would take longer than the
+// work, and an item's place alone says whose it is (some then have none).
+__device__ __forceinline__ bool find_item(const AttendArgs &a, uint32_t at, Item *it) {
+  const uint32_t item = at / a.c.n_heads;
+  it->h = at - item * a.c.n_heads;
+  uint32_t k = 0;
+  if (a.n_requests > 512) {
+    const Places pl = {a.q_start, a.n_requests, a.group, a.plan.rows, 1u};
+    const uint32_t place = item / a.plan.splits;
+    it->r = __builtin_amdgcn_readfirstlane(pl.find(place));
+    it->x = uniform(request_of(a, it->r, threadIdx.x == 0));
+    const uint32_t tile = place - __builtin_amdgcn_readfirstlane((uint32_t)pl.first(it->r));
+    k = tile * it->x.parts + item % a.plan.splits;
+    if (tile >= it->x.tiles || item % a.plan.splits >= it->x.parts) return false;
+  } else {
+    uint32_t base = 0;
+    for (uint32_t r0 = 0;; r0 += 64) {
+      if (r0 >= a.n_requests) return false;
+      const uint32_t r = r0 + lane_id();
+      Request x = {};
+      if (r < a.n_requests) x = request_of(a, r, threadIdx.x < 64 && at == 0);
+      const uint32_t n = x.tiles * x.parts;
+      uint32_t sum = n;
+      for (int i = 1; i < 64; i <<= 1) {
+        const uint32_t y = __shfl_up(sum, i);
+        if (lane_id() >= i) sum += y;
+      }
+      const uint32_t all = __builtin_amdgcn_readlane(sum, 63);
+      if (item - base < all) {
+        const uint32_t i = (uint32_t)__popcll(__ballot(sum <= item - base));
+        it->r = r0 + i;
+        it->x = from_lane(x, i);
+        k = item - base - (__builtin_amdgcn_readlane(sum, i) - __builtin_amdgcn_readlane(n, i));
+        break;
+      }
+      base += all;
+    }
+  }
+  it->tile = it->x.tiles - 1 - k / it->x.parts;
+  it->part = it->x.part0 + k % it->x.parts;
+  return true;
+}
+
 struct Yes {
   static constexpr bool value = true;
 };
@@ -550,14 +604,11 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   __shared__ u32x4 kf[2][8 * KC][64];  // [step][4 tiles x 2 KC][lane]
   __shared__ u32x4 vf[2][2 * VT][64];
   __shared__ uint32_t special[2][kWaves];
-  __shared__ Items items;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   const int c16 = lane & 15, g = lane >> 4, ka = c16 >> 2, kb = c16 & 3;
   const uint32_t bt = 1u << a.bt_log2;
-  ItemWalk walk;
-  walk.scan(a, &items);
   Item it;
-  if (!walk.find(a, &items, blockIdx.x, &it)) return;
+  if (!find_item(a, blockIdx.x, &it)) return;
   const Request &x = it.x;
   const Tile t = tile_of(a, x, it.tile);
   const bool none = t.part0 == t.part1;
@@ -597,10 +648,12 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const uint8_t *vbase = (const uint8_t *)a.c.v + ((uint64_t)h * D + 16 * wave + c16) * bt;
   const int32_t *row = a.table + (uint64_t)it.r * a.table_stride;
   bool bad_page = false;
-  auto block_of = [&](uint32_t j) -> int32_t {
-    const bool in = j < t.hi && j + 16 > t.lo;
-    const int32_t id = row[(in ? j : t.lo) >> a.bt_log2];
-    const bool out = in && (uint32_t)id >= a.c.n_blocks;
+  // the table's entry for token j (a multiple of 16), and the block that it is:
+  // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
+  // when it is needed: looking at once would wait for it.)
+  auto entry_of = [&](uint32_t j) { return row[(j < t.hi && j + 16 > t.lo ? j : t.lo) >> a.bt_log2]; };
+  auto block_of = [&](int32_t id, uint32_t j) -> int32_t {
+    const bool in = j < t.hi && j + 16 > t.lo, out = in && (uint32_t)id >= a.c.n_blocks;
     bad_page |= out;
     return in && !out ? id : -1;
   };
@@ -609,19 +662,20 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   auto has_v = [&](int j) { return VT % kWaves == 0 || wave + kWaves * j < VT; };
   u32x4 kg[KW], vg[VW];
   float ks1 = 0.0f, vs1 = 0.0f;
-  int32_t idk1 = -1, idv1 = -1, idk2 = -1, idv2 = -1;  // of the step that is loaded, and of the one after
+  int32_t idk1 = -1, idv1 = -1;  // blocks of the step that is loaded
+  int32_t ek = 0, ev = 0;        // entries of the one after
   auto blocks = [&](uint32_t s) {
-    idk2 = block_of((s << 6) + 16 * ka);
-    idv2 = block_of((s << 6) + 16 * g);
+    ek = entry_of((s << 6) + 16 * ka);
+    ev = entry_of((s << 6) + 16 * g);
   };
   auto load = [&](uint32_t s) {
     const uint32_t t0 = s << 6;
-    const uint8_t *kp = kbase + (uint64_t)(idk2 < 0 ? 0 : idk2) * a.c.k_stride +
+    idk1 = block_of(ek, t0 + 16 * ka);
+    idv1 = block_of(ev, t0 + 16 * g);
+    const uint8_t *kp = kbase + (uint64_t)(idk1 < 0 ? 0 : idk1) * a.c.k_stride +
                         ((t0 + 16 * ka) & (bt - 1)) * D;
-    const uint8_t *vp = vbase + (uint64_t)(idv2 < 0 ? 0 : idv2) * a.c.v_stride +
+    const uint8_t *vp = vbase + (uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_stride +
                         ((t0 + 16 * g) & (bt - 1));
-    idk1 = idk2;
-    idv1 = idv2;
 #pragma unroll
     for (int j = 0; j < KW; ++j)
       if (has_k(j)) kg[j] = *(const u32x4 *)(kp + j * KS * 64);
@@ -674,7 +728,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     }
     // the values' unit is the largest scale so far
     vref = fmaxf(vref, group_max(vs));
-    const float ratio = fmaxf(vs / vref, 0x1p-60f);
+    const float ratio = fmaxf(vs * __builtin_amdgcn_rcpf(vref), 0x1p-60f);
     __syncthreads();
     const int t0 = (int)(s << 6);
     if (kMasked) {
@@ -730,10 +784,11 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     bool grows = w.vref != vref;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      float y = sc[n][0][0];
+      float y = max3(sc[n][0][0], sc[n][0][1], sc[n][0][2]);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) y = fmaxf(y, sc[n][i >> 2][i & 3]);
-      y *= f;
+      for (int i = 3; i < 15; i += 2)
+        y = max3(y, sc[n][i >> 2][i & 3], sc[n][(i + 1) >> 2][(i + 1) & 3]);
+      y = max3(y, sc[n][3][3], sc[n][3][3]) * f;
       top[n] = group_max(!kMasked && idv < 0 ? kNegInf : y);
       grows |= top[n] > w.m[n] + kSlack;
     }
@@ -750,7 +805,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
         for (int i = 0; i < VT; ++i) w.o[n][i] *= keep * shrink;
       }
     }
-    const float back = 1.0f / ratio, lift = kLiftMany + __builtin_amdgcn_logf(ratio);
+    const float back = __builtin_amdgcn_rcpf(ratio), lift = kLiftMany + __builtin_amdgcn_logf(ratio);
     f16x8 p[NQ][2], p_low[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
