@@ -107,15 +107,6 @@ __device__ __forceinline__ uint32_t take_special(u32x4 &x, int j) {
   return sp;
 }
 
-template <int DT>
-__device__ __forceinline__ float load_elem(const void *p, uint64_t i) {
-  if (DT == WM_BF16)
-    return __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16);
-  return (float)static_cast<const _Float16 *>(p)[i];
-}
-
-// ---- attention ----------------------------------------------------------------
-
 // A request as attention sees it.  Its query rows that share a key head are its
 // tokens times the heads of the group, row = token * group + head; tiles of
 // `rows` of them are worked on together.  Its sequence is cut into parts of 2^cut tokens

@@ -17,131 +17,162 @@ namespace {
 // tokens lie; the writes are then divided over the grid.  No workgroup waits
 // for another.  What is written is never read by the same call: taken and
 // returned places of the ring are disjoint (count + returns <= capacity), and
-// a table entry is read only where it was in use before.
-constexpr int kTabThreads = 1024;
-
+// a table entry is read only where it was in use before.  256 or 2048 requests
+// need one scan, more a first pass for the totals.
+// What bounds it: the chain lengths - scan - search - ring - store for a
+// step, the 8 bytes a token for an admission.
 struct Step {
-  int32_t o, n;
-  uint32_t b, c, tokens, need, give;
+  int32_t o, n;   // lengths and
+  uint32_t b, c;  // blocks before and after
+  __device__ __forceinline__ uint32_t tokens() const { return n > o ? (uint32_t)(n - o) : 0u; }
+  __device__ __forceinline__ uint32_t need() const { return c > b ? c - b : 0u; }
+  __device__ __forceinline__ uint32_t give() const { return b > c ? b - c : 0u; }
+  __device__ __forceinline__ bool bad(const TablesArgs &a) const {
+    return o < 0 || n < 0 || b > a.max_blocks || c > a.max_blocks;
+  }
 };
 
 __device__ __forceinline__ Step step_of(const TablesArgs &a, uint32_t r) {
-  Step s = {0, 0, 0, 0, 0, 0, 0};
+  Step s = {0, 0, 0, 0};
   if (r >= a.n_requests) return s;
   s.o = a.old_len[r];
   s.n = a.new_len[r];
   const uint32_t round = (1u << a.bt_log2) - 1u;
-  // a negative length becomes a large count that fails the check
   s.b = (uint32_t)(((uint64_t)(uint32_t)s.o + round) >> a.bt_log2);
   s.c = (uint32_t)(((uint64_t)(uint32_t)s.n + round) >> a.bt_log2);
-  s.tokens = s.n > s.o ? (uint32_t)(s.n - s.o) : 0u;
-  s.need = s.c > s.b ? s.c - s.b : 0u;
-  s.give = s.b > s.c ? s.b - s.c : 0u;
   return s;
 }
 
+// A thread scans PER neighbouring requests by itself before the waves do.
+constexpr int kTabThreads = 256;
+
+template <int PER>
 __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
-  __shared__ uint64_t sum[3][kTabThreads / 64];
-  __shared__ uint64_t pre[3][kTabThreads + 1];
-  __shared__ Step st[kTabThreads];
+  constexpr int NT = kTabThreads, kTile = NT * PER;
+  __shared__ uint64_t sum[3][NT / 64];
+  __shared__ uint32_t pre[3][kTile + 1];
+  __shared__ Step st[kTile];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const uint32_t head = a.pool_in[0], count = a.pool_in[1];
-  // pass 1: totals
-  uint64_t tok = 0, need = 0, give = 0;
-  bool bad = false;
-  for (uint32_t r = tid; r < a.n_requests; r += kTabThreads) {
-    const Step s = step_of(a, r);
-    bad |= s.o < 0 || s.n < 0 || s.b > a.max_blocks || s.c > a.max_blocks;
-    tok += s.tokens;
-    need += s.need;
-    give += s.give;
+  // tokens, blocks taken and blocks returned in all
+  uint64_t total[3] = {0, 0, 0};
+  auto decide = [&](bool bad) -> bool {
+    uint32_t v = 0;
+    if (total[1] > count || count + total[2] > a.ring_cap || head >= a.ring_cap) v |= WM_C_POOL;
+    if (total[0] > a.slot_cap) v |= WM_C_SLOTS;
+    if (bad) v = WM_C_LENGTH;  // the other counts mean nothing then
+    if (blockIdx.x == 0 && tid == 0) {
+      *a.verdict = v;
+      a.pool_out[0] = v ? head : (uint32_t)((head + total[1]) % a.ring_cap);
+      a.pool_out[1] = v ? count : (uint32_t)(count - total[1] + total[2]);
+      if (!v) a.q_start[a.n_requests] = (int32_t)total[0];
+    }
+    return v == 0;
+  };
+  const bool once = a.n_requests <= kTile;
+  if (!once) {
+    uint64_t x[3] = {0, 0, 0};
+    bool bad = false;
+    for (uint32_t r = tid; r < a.n_requests; r += NT) {
+      const Step s = step_of(a, r);
+      bad |= s.bad(a);
+      x[0] += s.tokens();
+      x[1] += s.need();
+      x[2] += s.give();
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      for (int i = 32; i; i >>= 1) x[k] += __shfl_xor(x[k], i);
+      if (lane == 0) sum[k][wave] = x[k];
+    }
+    bad = __syncthreads_or(bad);
+    for (int k = 0; k < 3; ++k)
+      for (int i = 0; i < NT / 64; ++i) total[k] += sum[k][i];
+    if (!decide(bad)) return;
   }
-  for (int i = 32; i; i >>= 1) {
-    tok += __shfl_xor(tok, i);
-    need += __shfl_xor(need, i);
-    give += __shfl_xor(give, i);
-  }
-  if (lane == 0) {
-    sum[0][wave] = tok;
-    sum[1][wave] = need;
-    sum[2][wave] = give;
-  }
-  bad = __syncthreads_or(bad);
-  tok = need = give = 0;
-  for (int i = 0; i < kTabThreads / 64; ++i) {
-    tok += sum[0][i];
-    need += sum[1][i];
-    give += sum[2][i];
-  }
-  uint32_t v = 0;
-  if (need > count || count + give > a.ring_cap || head >= a.ring_cap) v |= WM_C_POOL;
-  if (tok > a.slot_cap) v |= WM_C_SLOTS;
-  if (bad) v = WM_C_LENGTH;  // the other counts mean nothing then
-  if (blockIdx.x == 0 && tid == 0) {
-    *a.verdict = v;
-    a.pool_out[0] = v ? head : (uint32_t)((head + need) % a.ring_cap);
-    a.pool_out[1] = v ? count : (uint32_t)(count - need + give);
-    if (!v) a.q_start[a.n_requests] = (int32_t)tok;
-  }
-  if (v) return;
-  // pass 2: a tile of requests at a time
-  const uint64_t step = (uint64_t)gridDim.x * kTabThreads;
-  const uint64_t at = (uint64_t)blockIdx.x * kTabThreads + tid;
+  const uint64_t step = (uint64_t)gridDim.x * NT;
+  const uint64_t at = (uint64_t)blockIdx.x * NT + tid;
   const uint32_t bt = 1u << a.bt_log2;
+  // a place of the ring: less than two rounds
+  auto place = [&](uint64_t x) { return (uint32_t)(x >= a.ring_cap ? x - a.ring_cap : x); };
   uint64_t base[3] = {0, 0, 0};
-  for (uint32_t r0 = 0; r0 < a.n_requests; r0 += kTabThreads) {
+  for (uint32_t r0 = 0; r0 < a.n_requests || (once && r0 == 0); r0 += kTile) {
     __syncthreads();  // the tile before is done with the shared arrays
-    const uint32_t r = r0 + tid;
-    const Step s = step_of(a, r);
-    st[tid] = s;
-    uint64_t x[3] = {s.tokens, s.need, s.give};
+    Step s[PER];
+    uint64_t x[3] = {0, 0, 0};
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) s[i] = step_of(a, r0 + PER * tid + i);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      st[PER * tid + i] = s[i];
+      bad |= s[i].bad(a);
+      x[0] += s[i].tokens();
+      x[1] += s[i].need();
+      x[2] += s[i].give();
+    }
+    const uint64_t own[3] = {x[0], x[1], x[2]};
     for (int i = 1; i < 64; i <<= 1)
+#pragma unroll
       for (int k = 0; k < 3; ++k) {
         const uint64_t y = __shfl_up(x[k], i);
         if (lane >= i) x[k] += y;
       }
     if (lane == 63)
+#pragma unroll
       for (int k = 0; k < 3; ++k) sum[k][wave] = x[k];
-    __syncthreads();
+    bad = __syncthreads_or(bad);
+#pragma unroll
     for (int k = 0; k < 3; ++k) {
-      uint64_t w = base[k];
-      for (int i = 0; i < wave; ++i) w += sum[k][i];
-      pre[k][tid + 1] = w + x[k];
-      if (tid == 0) pre[k][0] = base[k];
-    }
-    __syncthreads();
-    if (blockIdx.x == 0 && r < a.n_requests) a.q_start[r] = (int32_t)pre[0][tid];
-    auto owner = [&](int k, uint64_t j) {  // the last request whose part begins at or before j
-      int lo = 0, hi = kTabThreads;
-      while (hi - lo > 1) {
-        const int m = (lo + hi) >> 1;
-        if (pre[k][m] <= j)
-          lo = m;
-        else
-          hi = m;
+      uint64_t before = base[k], all = base[k];
+#pragma unroll
+      for (int i = 0; i < NT / 64; ++i) {
+        if (i < wave) before += sum[k][i];
+        all += sum[k][i];
       }
+      // (32 bits: enough once decide() has passed)
+      uint32_t p = (uint32_t)(before + x[k] - own[k]);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        pre[k][PER * tid + i] = p;
+        p += k == 0 ? s[i].tokens() : (k == 1 ? s[i].need() : s[i].give());
+      }
+      if (tid == NT - 1) pre[k][kTile] = p;
+      if (once) total[k] = all;
+      base[k] = all;
+    }
+    if (once && !decide(bad)) return;
+    __syncthreads();
+    if (blockIdx.x == 0)
+      for (uint32_t i = tid; i < kTile && r0 + i < a.n_requests; i += NT)
+        a.q_start[r0 + i] = (int32_t)pre[0][i];
+    auto owner = [&](int k, uint32_t j) {  // the last request whose part begins at or before j
+      int lo = 0;
+#pragma unroll
+      for (int m = kTile / 2; m; m >>= 1)
+        if (pre[k][lo + m] <= j) lo += m;
       return lo;
     };
-    for (uint64_t j = pre[1][0] + at; j < pre[1][kTabThreads]; j += step) {
-      const int i = owner(1, j);
-      a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].b + (uint32_t)(j - pre[1][i])] =
-          a.ring[(head + j) % a.ring_cap];
+    for (uint64_t j = pre[1][0] + at; j < pre[1][kTile]; j += step) {
+      const int i = owner(1, (uint32_t)j);
+      a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].b + ((uint32_t)j - pre[1][i])] =
+          a.ring[place(head + j)];
     }
-    for (uint64_t j = pre[2][0] + at; j < pre[2][kTabThreads]; j += step) {
-      const int i = owner(2, j);
-      a.ring[(head + count + j) % a.ring_cap] =
-          a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].c + (uint32_t)(j - pre[2][i])];
+    for (uint64_t j = pre[2][0] + at; j < pre[2][kTile]; j += step) {
+      const int i = owner(2, (uint32_t)j);
+      a.ring[place((uint64_t)place((uint64_t)head + count) + j)] =
+          a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].c + ((uint32_t)j - pre[2][i])];
     }
-    for (uint64_t j = pre[0][0] + at; j < pre[0][kTabThreads]; j += step) {
-      const int i = owner(0, j);
-      const uint32_t p = (uint32_t)st[i].o + (uint32_t)(j - pre[0][i]);
+#pragma unroll 4
+    for (uint64_t j = pre[0][0] + at; j < pre[0][kTile]; j += step) {
+      const int i = owner(0, (uint32_t)j);
+      const uint32_t p = (uint32_t)st[i].o + ((uint32_t)j - pre[0][i]);
       const uint32_t blk = p >> a.bt_log2;
       const int32_t id = blk < st[i].b
                              ? a.table[(uint64_t)(r0 + i) * a.table_stride + blk]
-                             : a.ring[(head + pre[1][i] + (blk - st[i].b)) % a.ring_cap];
+                             : a.ring[place((uint64_t)head + pre[1][i] + (blk - st[i].b))];
       a.slots[j] = (int64_t)id * bt + (p & (bt - 1u));
     }
-    for (int k = 0; k < 3; ++k) base[k] = pre[k][kTabThreads];
   }
 }
 
@@ -163,23 +194,67 @@ __device__ __forceinline__ float raise_scale(float was, float amax, bool fresh) 
   return (float)ldexp(base, k);
 }
 
+// Four codes.  x / scale is rounded only where the caller's own scale, no power
+// of two, is kept; inv is 1 / scale where that is exact, else 0.
 template <int FMT>
-__device__ __forceinline__ uint32_t code_of(float x, float scale) {
-  float y = x / scale;  // a power of two unless the caller's own scale is kept: then rounded
+__device__ __forceinline__ uint32_t codes_of(const float *x, float scale, float inv) {
   const float big = Code<FMT>::kLargest;
-  y = y > big ? big : (y < -big ? -big : y);  // NaN passes
-  return Code<FMT>::two(y, 0.0f) & 0xFFu;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = inv != 0.0f ? x[i] * inv : x[i] / scale;
+    y[i] = y[i] > big ? big : (y[i] < -big ? -big : y[i]);  // NaN passes
+  }
+  return Code<FMT>::two(y[0], y[1]) | Code<FMT>::two(y[2], y[3]) << 16;
 }
 
-// A workgroup takes one block that gets tokens, one head, keys or values:
-// the largest magnitude first, then the codes.  Keys are stored as they come,
-// values transposed.
-template <int DT, int FMT>
+// Four codes whose scale was raised by 1 / ratio, a power of two.
+template <int FMT>
+__device__ __forceinline__ uint32_t moved_codes(uint32_t w, float ratio) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = Code<FMT>::value(w >> (8 * i) & 0xFFu) * ratio;
+  return Code<FMT>::two(y[0], y[1]) | Code<FMT>::two(y[2], y[3]) << 16;
+}
+
+// Eight neighbouring elements of a row.
+template <int DT, bool WIDE>
+__device__ __forceinline__ void load_eight(const void *p, uint64_t at, float *x) {
+  const uint16_t *e = static_cast<const uint16_t *>(p) + at;
+  u32x4 w;
+  if (WIDE) {
+    w = *(const u32x4 *)e;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t h = w[i >> 1] >> (16 * (i & 1)) & 0xFFFFu;
+    x[i] = DT == WM_BF16 ? __uint_as_float(h << 16)
+                         : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+  }
+}
+
+// A block that gets tokens, a head, keys or values: the largest magnitude
+// first, then the codes, from the same 16-byte loads (the second time from
+// L2).  NT threads work on it: a workgroup where blocks get many tokens, a wave where
+// they get a few (a step's single tokens: no barrier, and four times as many
+// blocks on their way).  Keys are stored as they come.  Values are
+// transposed in registers: a thread takes four tokens of eight dimensions and
+// stores eight words of four tokens, its neighbours the next four tokens, so
+// that 16 threads read 64 bytes of a row and write 64 bytes of one.  What
+// bounds it: HBM for prompts; for single tokens a chain of four loads (starts,
+// slot, row and scale, codes).
+template <int DT, int FMT, int NT, bool WIDE>
 __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
-  const uint32_t bt = 1u << a.bt_log2, dim = a.c.head_dim;
-  const int tid = threadIdx.x;
+  __shared__ float part[kAppThreads / 64];
+  const uint32_t bt = 1u << a.bt_log2, dim = a.c.head_dim, d8 = dim / 8;
+  const uint32_t tid = NT == 64 ? (uint32_t)lane_id() : threadIdx.x;
+  const uint32_t place = __builtin_amdgcn_readfirstlane(
+      NT == 64 ? blockIdx.x * (kAppThreads / 64) + (threadIdx.x >> 6) : blockIdx.x);
   const Places pl = {a.q_start, a.n_requests, 1u, bt, 2u};
-  const uint32_t r = pl.find(blockIdx.x);
+  const uint32_t r = __builtin_amdgcn_readfirstlane(pl.find(place));
   const uint32_t h = blockIdx.y;
   const bool value = blockIdx.z != 0;
   int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1];
@@ -187,7 +262,7 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
     if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_SLOTS);
     q1 = a.n_tokens;
   }
-  const int64_t nth = (int64_t)blockIdx.x - pl.first(r);
+  const int64_t nth = (int64_t)place - pl.first(r);
   if (q0 < 0 || nth < 0 || q0 >= q1) return;
   // the block's tokens: nth * bt - at .. of the request's, at being the place
   // of the first new token in its block
@@ -198,7 +273,7 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   int64_t end = q0 + (nth + 1) * bt - at;
   end = end < q1 ? end : q1;
   const uint32_t off = nth ? 0u : (uint32_t)at, n_new = (uint32_t)(end - begin);
-  const int64_t slot = a.slots[begin];
+  const int64_t slot = nth ? a.slots[begin] : s0;
   if (slot < 0) return;
   const uint64_t page = (uint64_t)slot >> a.bt_log2;
   if (page >= a.c.n_blocks) {
@@ -208,41 +283,96 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   const bool fresh = off == 0;
   const wm_rows &src = value ? a.v : a.k;
   const uint64_t row0 = (uint64_t)begin * src.row_stride + (uint64_t)h * src.head_stride;
-  const uint32_t n_elem = n_new * dim;
-  float amax = 0.0f;
-  for (uint32_t i = tid; i < n_elem; i += kAppThreads) {
-    const float x = fabsf(load_elem<DT>(src.ptr, row0 + (uint64_t)(i / dim) * src.row_stride + i % dim));
-    if (x <= 3.4028234e38f && x > amax) amax = x;
-  }
-  __shared__ float part[kAppThreads / 64];
-  for (int i = 32; i; i >>= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
-  if ((tid & 63) == 0) part[tid >> 6] = amax;
-  __syncthreads();
-  for (int i = 0; i < kAppThreads / 64; ++i) amax = fmaxf(amax, part[i]);
   float *sp = (value ? a.c.v_scale + page * a.c.v_scale_stride
                      : a.c.k_scale + page * a.c.k_scale_stride) + h;
   const float was = *sp;
+  float amax = 0.0f;
+  for (uint32_t i = tid; i < n_new * d8; i += NT) {
+    float x[8];
+    load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(i / d8) * src.row_stride + i % d8 * 8, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float y = fabsf(x[j]);
+      if (y <= 3.4028234e38f && y > amax) amax = y;
+    }
+  }
+  for (int i = 32; i; i >>= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
+  if (NT > 64) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = amax;
+    __syncthreads();  // (and every thread has read the scale)
+    for (int i = 0; i < kAppThreads / 64; ++i) amax = fmaxf(amax, part[i]);
+  }
   const float now = raise_scale<FMT>(was, amax, fresh);
-  __syncthreads();  // every thread has read the scale
   if (tid == 0 && now != was) *sp = now;
-  uint8_t *codes = value ? (uint8_t *)a.c.v + page * a.c.v_stride : (uint8_t *)a.c.k + page * a.c.k_stride;
-  codes += (uint64_t)h * bt * dim;
+  const float inv = (__float_as_uint(now) & 0x7FFFFFu) == 0 ? 1.0f / now : 0.0f;
   const bool again = !fresh && now != was;
   const float ratio = again ? was / now : 1.0f;
-  for (uint32_t i = tid; i < bt * dim; i += kAppThreads) {
-    const uint32_t t = value ? i & (bt - 1) : i / dim;  // token of the block
-    const uint32_t d = value ? i >> a.bt_log2 : i % dim;
-    uint32_t b;
-    if (t >= off && t < off + n_new) {
-      b = code_of<FMT>(load_elem<DT>(src.ptr, row0 + (uint64_t)(t - off) * src.row_stride + d), now);
-    } else if (fresh) {
-      b = 0;
-    } else if (again) {
-      b = Code<FMT>::two(Code<FMT>::value(codes[i]) * ratio, 0.0f) & 0xFFu;
-    } else {
-      continue;
+  const uint64_t base = (uint64_t)h * bt * dim;
+  if (!value) {
+    uint8_t *codes = (uint8_t *)a.c.k + page * a.c.k_stride + base;
+    // only the new rows, unless all of the block's change
+    const bool all = fresh || again;
+    const uint32_t t0 = all ? 0u : off, t1 = all ? bt : off + n_new;
+    for (uint32_t i = t0 * d8 + tid; i < t1 * d8; i += NT) {
+      const uint32_t t = i / d8;
+      u32x2 *to = (u32x2 *)(codes + (uint64_t)i * 8);
+      u32x2 w = {0, 0};
+      if (t >= off && t < off + n_new) {
+        float x[8];
+        load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(t - off) * src.row_stride + i % d8 * 8, x);
+        w = u32x2{codes_of<FMT>(x, now, inv), codes_of<FMT>(x + 4, now, inv)};
+      } else if (again) {
+        const u32x2 y = *to;
+        w = u32x2{moved_codes<FMT>(y[0], ratio), moved_codes<FMT>(y[1], ratio)};
+      }
+      *to = w;
     }
-    codes[i] = (uint8_t)b;
+    return;
+  }
+  uint8_t *codes = (uint8_t *)a.c.v + page * a.c.v_stride + base;
+  const bool all = fresh || again;
+  const uint32_t g0 = all ? 0u : off / 4, g1 = all ? bt / 4 : (off + n_new + 3) / 4;  // groups of four tokens
+  const uint32_t ng = g1 - g0;
+  for (uint32_t i = tid; i < ng * d8; i += NT) {
+    const uint32_t t = (g0 + i % ng) * 4, d = i / ng * 8;
+    uint32_t *to = (uint32_t *)(codes + (uint64_t)d * bt + t);
+    uint32_t w[8], mine = 0;  // mine: bytes of the words that are new tokens
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (t + j >= off && t + j < off + n_new) mine |= 0xFFu << (8 * j);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = 0;
+    if (!fresh && mine != ~0u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        w[j] = to[(uint64_t)j * (bt / 4)];
+        if (again) w[j] = moved_codes<FMT>(w[j], ratio);
+      }
+    }
+    if (mine) {
+      uint32_t c[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // a place that gets no token takes its codes from one that does; they
+        // are not used
+        uint32_t tok = t + j < off ? off : t + j;
+        tok = tok < off + n_new ? tok - off : n_new - 1;
+        float x[8];
+        load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)tok * src.row_stride + d, x);
+        c[j][0] = codes_of<FMT>(x, now, inv);
+        c[j][1] = codes_of<FMT>(x + 4, now, inv);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = j >> 2, sel = j & 3;
+        // byte sel of four words into one
+        const uint32_t lo = __builtin_amdgcn_perm(c[1][k], c[0][k], 0x0C0C0400u + 0x0101u * sel);
+        const uint32_t hi = __builtin_amdgcn_perm(c[3][k], c[2][k], 0x0C0C0400u + 0x0101u * sel);
+        w[j] = (w[j] & ~mine) | ((lo | hi << 16) & mine);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[(uint64_t)j * (bt / 4)] = w[j];
   }
 }
 
@@ -354,27 +484,49 @@ int last_error() { return (int)hipGetLastError(); }
 }  // namespace
 
 int launch_page_tables(const TablesArgs &a, void *stream) {
-  // a workgroup for each 4096 slots, at most two per CU
-  uint64_t n = (a.slot_cap + 4095) / 4096;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  // a workgroup for each 2048 slots (512 where there are few), at most as many
+  // as 256 CUs hold at once (57 KiB of LDS each); one scan for up to 256 or
+  // 2048 requests
+  const uint64_t per = a.slot_cap <= 8192 ? 512 : 2048;
+  uint64_t n = (a.slot_cap + per - 1) / per;
   n = n < 1 ? 1 : (n > 512 ? 512 : n);
-  k_page_tables<<<(uint32_t)n, kTabThreads, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  if (a.n_requests <= 256)
+    k_page_tables<1><<<(uint32_t)n, kTabThreads, 0, st>>>(a);
+  else
+    k_page_tables<8><<<(uint32_t)n, kTabThreads, 0, st>>>(a);
   return last_error();
 }
 
+namespace {
+
+template <int DT, int FMT>
+int append_types(const AppendArgs &a, hipStream_t st) {
+  const uint32_t places = (a.n_tokens >> a.bt_log2) + 2u * a.n_requests;
+  // a wave for a block's few tokens: up to eight a request on average
+  const bool few = a.n_tokens <= 8ull * a.n_requests;
+  const bool wide = (((uintptr_t)a.k.ptr >> 1 | (uintptr_t)a.v.ptr >> 1 | a.k.row_stride |
+                      a.k.head_stride | a.v.row_stride | a.v.head_stride) & 7u) == 0;
+  const dim3 grid(few ? (places + 3) / 4 : places, a.c.n_heads, 2);
+  if (few && wide)
+    k_cache_append<DT, FMT, 64, true><<<grid, kAppThreads, 0, st>>>(a);
+  else if (few)
+    k_cache_append<DT, FMT, 64, false><<<grid, kAppThreads, 0, st>>>(a);
+  else if (wide)
+    k_cache_append<DT, FMT, kAppThreads, true><<<grid, kAppThreads, 0, st>>>(a);
+  else
+    k_cache_append<DT, FMT, kAppThreads, false><<<grid, kAppThreads, 0, st>>>(a);
+  return last_error();
+}
+
+}  // namespace
+
 int launch_cache_append(const AppendArgs &a, void *stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  const uint32_t places = (a.n_tokens >> a.bt_log2) + 2u * a.n_requests;
-  const dim3 grid(places, a.c.n_heads, 2);
   const bool e4 = a.c.format == WM_E4M3;
-  if (a.k.dtype == WM_BF16 && e4)
-    k_cache_append<WM_BF16, WM_E4M3><<<grid, kAppThreads, 0, st>>>(a);
-  else if (a.k.dtype == WM_BF16)
-    k_cache_append<WM_BF16, WM_E5M2><<<grid, kAppThreads, 0, st>>>(a);
-  else if (e4)
-    k_cache_append<WM_FP16, WM_E4M3><<<grid, kAppThreads, 0, st>>>(a);
-  else
-    k_cache_append<WM_FP16, WM_E5M2><<<grid, kAppThreads, 0, st>>>(a);
-  return last_error();
+  if (a.k.dtype == WM_BF16)
+    return e4 ? append_types<WM_BF16, WM_E4M3>(a, st) : append_types<WM_BF16, WM_E5M2>(a, st);
+  return e4 ? append_types<WM_FP16, WM_E4M3>(a, st) : append_types<WM_FP16, WM_E5M2>(a, st);
 }
 
 int launch_cache_attend(const AttendArgs &a, void *stream) {
