@@ -59,7 +59,7 @@ extern "C" {
  * The strides are those from a block to the next (codes: bytes, a multiple
  * of 16; scales: floats), so that one pool may hold every layer's blocks side
  * by side; everything inside a block is dense.  k and v are 16-byte aligned.
- * Scales are finite. */
+ * Scales are finite and not negative. */
 typedef struct wm_cache {
   void *k, *v;
   float *k_scale, *v_scale;
@@ -124,7 +124,8 @@ wm_status wm_page_tables(const int32_t *old_len, const int32_t *new_len,
  * in order, and slot_map says where each is stored (wm_page_tables).  For each
  * block and head that gets tokens, with F the format's largest value and a the
  * largest finite magnitude of what it gets (keys and values apart):
- *   a block whose first place gets a token is fresh: its scale becomes 2^e
+ *   a block whose first place gets a token, or whose scale is no positive
+ *   finite (and normal) number, is fresh: its scale becomes 2^e
  *   with the smallest e >= -100 such that a <= F 2^e, and its places that
  *   get no token become zero;
  *   any other block keeps its scale s if a <= F s, else the scale becomes

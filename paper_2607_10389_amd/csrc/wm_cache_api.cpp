@@ -89,7 +89,8 @@ wm_status pages_call(bool gather, const wm_pool *pools, uint32_t n_pools, const 
   if (!total) return WM_OK;
   const int n_cu = cus();
   if (!n_cu) return WM_ERR_HIP;
-  if (launch_check_pages(pages, n_pages, least, verdict, stream) != 0) return WM_ERR_HIP;
+  if (n_pages > kPagesLooked && launch_check_pages(pages, n_pages, least, verdict, stream) != 0)
+    return WM_ERR_HIP;
   uint64_t off = 0;
   for (uint32_t i = 0; i < n_pools;) {
     PoolBatch b;

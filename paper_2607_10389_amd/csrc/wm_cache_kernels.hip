@@ -179,6 +179,7 @@ __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
 // ---- store new keys and values -----------------------------------------------
 
 constexpr int kAppThreads = 256;
+constexpr uint32_t kPlacesY = 32768;  // a grid's second axis
 
 // The scale of a block that gets values of magnitude up to amax.  448 = 0.875
 // 2^9 and 57344 = 0.875 2^16, and products with a 24-bit scale are exact in
@@ -194,15 +195,14 @@ __device__ __forceinline__ float raise_scale(float was, float amax, bool fresh) 
   return (float)ldexp(base, k);
 }
 
-// Four codes.  x / scale is rounded only where the caller's own scale, no power
-// of two, is kept; inv is 1 / scale where that is exact, else 0.
+// Four codes; inv: 1 / scale, a power of two, so that the product is exact.
 template <int FMT>
-__device__ __forceinline__ uint32_t codes_of(const float *x, float scale, float inv) {
+__device__ __forceinline__ uint32_t codes_of(const float *x, float inv) {
   const float big = Code<FMT>::kLargest;
   float y[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[i] = inv != 0.0f ? x[i] * inv : x[i] / scale;
+    y[i] = x[i] * inv;
     y[i] = y[i] > big ? big : (y[i] < -big ? -big : y[i]);  // NaN passes
   }
   return Code<FMT>::two(y[0], y[1]) | Code<FMT>::two(y[2], y[3]) << 16;
@@ -215,6 +215,11 @@ __device__ __forceinline__ uint32_t moved_codes(uint32_t w, float ratio) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = Code<FMT>::value(w >> (8 * i) & 0xFFu) * ratio;
   return Code<FMT>::two(y[0], y[1]) | Code<FMT>::two(y[2], y[3]) << 16;
+}
+
+template <int DT>
+__device__ __forceinline__ float element(uint16_t h) {
+  return DT == WM_BF16 ? __uint_as_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
 }
 
 // Eight neighbouring elements of a row.
@@ -231,8 +236,7 @@ __device__ __forceinline__ void load_eight(const void *p, uint64_t at, float *x)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t h = w[i >> 1] >> (16 * (i & 1)) & 0xFFFFu;
-    x[i] = DT == WM_BF16 ? __uint_as_float(h << 16)
-                         : (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+    x[i] = element<DT>((uint16_t)h);
   }
 }
 
@@ -251,12 +255,15 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   __shared__ float part[kAppThreads / 64];
   const uint32_t bt = 1u << a.bt_log2, dim = a.c.head_dim, d8 = dim / 8;
   const uint32_t tid = NT == 64 ? (uint32_t)lane_id() : threadIdx.x;
+  // neighbouring workgroups take neighbouring heads: of a token's row they
+  // read one stretch
+  const uint32_t unit = blockIdx.z * kPlacesY + blockIdx.y;
   const uint32_t place = __builtin_amdgcn_readfirstlane(
-      NT == 64 ? blockIdx.x * (kAppThreads / 64) + (threadIdx.x >> 6) : blockIdx.x);
+      NT == 64 ? unit * (kAppThreads / 64) + (threadIdx.x >> 6) : unit);
   const Places pl = {a.q_start, a.n_requests, 1u, bt, 2u};
   const uint32_t r = __builtin_amdgcn_readfirstlane(pl.find(place));
-  const uint32_t h = blockIdx.y;
-  const bool value = blockIdx.z != 0;
+  const bool value = blockIdx.x >= a.c.n_heads;
+  const uint32_t h = blockIdx.x - (value ? a.c.n_heads : 0u);
   int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1];
   if (q1 > (int64_t)a.n_tokens) {
     if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_SLOTS);
@@ -280,12 +287,12 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
     if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_PAGE);
     return;
   }
-  const bool fresh = off == 0;
   const wm_rows &src = value ? a.v : a.k;
   const uint64_t row0 = (uint64_t)begin * src.row_stride + (uint64_t)h * src.head_stride;
   float *sp = (value ? a.c.v_scale + page * a.c.v_scale_stride
                      : a.c.k_scale + page * a.c.k_scale_stride) + h;
   const float was = *sp;
+  const bool fresh = off == 0 || !(was >= 0x1p-126f && was <= 3.4028234e38f);
   float amax = 0.0f;
   for (uint32_t i = tid; i < n_new * d8; i += NT) {
     float x[8];
@@ -304,10 +311,29 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   }
   const float now = raise_scale<FMT>(was, amax, fresh);
   if (tid == 0 && now != was) *sp = now;
-  const float inv = (__float_as_uint(now) & 0x7FFFFFu) == 0 ? 1.0f / now : 0.0f;
   const bool again = !fresh && now != was;
   const float ratio = again ? was / now : 1.0f;
   const uint64_t base = (uint64_t)h * bt * dim;
+  if ((__float_as_uint(now) & 0x7FFFFFu) != 0) {
+    // the caller's own scale, no power of two: true quotients, a byte at a time
+    uint8_t *codes = value ? (uint8_t *)a.c.v + page * a.c.v_stride : (uint8_t *)a.c.k + page * a.c.k_stride;
+    codes += base;
+#pragma unroll 1
+    for (uint32_t i = tid; i < bt * dim; i += NT) {
+      const uint32_t t = value ? i & (bt - 1) : i / dim, d = value ? i >> a.bt_log2 : i % dim;
+      const uint16_t *e = (const uint16_t *)src.ptr + row0 + (uint64_t)(t - off) * src.row_stride + d;
+      if (t >= off && t < off + n_new) {
+        float y = element<DT>(*e) / now;
+        const float big = Code<FMT>::kLargest;
+        y = y > big ? big : (y < -big ? -big : y);
+        codes[i] = (uint8_t)Code<FMT>::two(y, 0.0f);
+      } else if (again) {
+        codes[i] = (uint8_t)Code<FMT>::two(Code<FMT>::value(codes[i]) * ratio, 0.0f);
+      }
+    }
+    return;
+  }
+  const float inv = 1.0f / now;
   if (!value) {
     uint8_t *codes = (uint8_t *)a.c.k + page * a.c.k_stride + base;
     // only the new rows, unless all of the block's change
@@ -320,7 +346,7 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
       if (t >= off && t < off + n_new) {
         float x[8];
         load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(t - off) * src.row_stride + i % d8 * 8, x);
-        w = u32x2{codes_of<FMT>(x, now, inv), codes_of<FMT>(x + 4, now, inv)};
+        w = u32x2{codes_of<FMT>(x, inv), codes_of<FMT>(x + 4, inv)};
       } else if (again) {
         const u32x2 y = *to;
         w = u32x2{moved_codes<FMT>(y[0], ratio), moved_codes<FMT>(y[1], ratio)};
@@ -359,8 +385,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
         tok = tok < off + n_new ? tok - off : n_new - 1;
         float x[8];
         load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)tok * src.row_stride + d, x);
-        c[j][0] = codes_of<FMT>(x, now, inv);
-        c[j][1] = codes_of<FMT>(x + 4, now, inv);
+        c[j][0] = codes_of<FMT>(x, inv);
+        c[j][1] = codes_of<FMT>(x + 4, inv);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -453,7 +479,18 @@ constexpr int kPageThreads = 256;
 template <bool GATHER, typename T>
 __global__ __launch_bounds__(kPageThreads) void k_pages(PoolBatch b, uint8_t *flat,
                                                         const int32_t *pages, uint32_t n_pages,
-                                                        const uint32_t *verdict) {
+                                                        uint64_t least, uint32_t *verdict) {
+  if (n_pages <= kPagesLooked) {
+    // every workgroup looks at the whole list, so that none writes if one
+    // block is bad
+    bool bad = false;
+    for (uint32_t i = threadIdx.x; i < n_pages; i += kPageThreads)
+      bad |= pages[i] < 0 || (uint64_t)pages[i] >= least;
+    if (__syncthreads_or(bad)) {
+      if (threadIdx.x == 0) atomicOr(verdict, WM_C_PAGE);
+      return;
+    }
+  }
   if (*verdict) return;
   for (uint64_t x = blockIdx.x; x < b.pieces; x += gridDim.x) {
     uint32_t lo = 0, hi = b.n;
@@ -507,7 +544,9 @@ int append_types(const AppendArgs &a, hipStream_t st) {
   const bool few = a.n_tokens <= 8ull * a.n_requests;
   const bool wide = (((uintptr_t)a.k.ptr >> 1 | (uintptr_t)a.v.ptr >> 1 | a.k.row_stride |
                       a.k.head_stride | a.v.row_stride | a.v.head_stride) & 7u) == 0;
-  const dim3 grid(few ? (places + 3) / 4 : places, a.c.n_heads, 2);
+  const uint32_t units = few ? (places + 3) / 4 : places;
+  const dim3 grid(2 * a.c.n_heads, units < kPlacesY ? units : kPlacesY,
+                  (units + kPlacesY - 1) / kPlacesY);
   if (few && wide)
     k_cache_append<DT, FMT, 64, true><<<grid, kAppThreads, 0, st>>>(a);
   else if (few)
@@ -566,17 +605,16 @@ int launch_pages(bool gather, const PoolBatch &b, uint8_t *flat, const int32_t *
                  uint32_t n_pages, uint64_t least_blocks, uint32_t *verdict, bool wide, int n_cu,
                  void *stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  (void)least_blocks;
   const uint64_t most = (uint64_t)n_cu * 8;
   const uint32_t grid = (uint32_t)(b.pieces < most ? b.pieces : most);
   if (gather && wide)
-    k_pages<true, u32x4><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, verdict);
+    k_pages<true, u32x4><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, least_blocks, verdict);
   else if (gather)
-    k_pages<true, uint32_t><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, verdict);
+    k_pages<true, uint32_t><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, least_blocks, verdict);
   else if (wide)
-    k_pages<false, u32x4><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, verdict);
+    k_pages<false, u32x4><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, least_blocks, verdict);
   else
-    k_pages<false, uint32_t><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, verdict);
+    k_pages<false, uint32_t><<<grid, kPageThreads, 0, st>>>(b, flat, pages, n_pages, least_blocks, verdict);
   return last_error();
 }
 
