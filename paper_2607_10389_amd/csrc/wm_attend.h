@@ -122,61 +122,49 @@ __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x
 
 // The work items of a call: a part of a tile of a request, for one key head.
 // They are counted on the device, by a scan over the requests' lengths that
-// every workgroup makes for itself, 256 requests at a time: lengths as
-// different as 1 and 100,000 in one call leave no workgroup without work.
-struct Items {
-  uint64_t pre[kAttThreads + 1], sums[kAttThreads / 64];
-  Request req[kAttThreads];
-};
-
+// every wave makes for itself, 64 requests at a time (a load, six shuffles and
+// no barrier): lengths as different as 1 and 100,000 in one call leave no
+// workgroup without work.
 struct Item {
   uint32_t r, h, tile, part;
   Request x;
 };
 
 struct ItemWalk {
-  uint64_t base = 0;  // items before the requests that are in LDS
-  uint32_t r0 = 0;
+  Request *mine;        // LDS: the wave's 64 requests
+  uint64_t base = 0;    // items before them
+  uint32_t r0 = 0, n = 0, sum = 0, all = 0;  // a lane's items, with those before it, all 64's
 
-  __device__ __forceinline__ void scan(const AttendArgs &a, Items *s) {
-    const int wave = threadIdx.x >> 6, lane = lane_id();
-    const uint32_t r = r0 + threadIdx.x;
+  __device__ __forceinline__ void scan(const AttendArgs &a) {
+    const uint32_t r = r0 + lane_id();
     Request x = {};
-    if (r < a.n_requests) x = request_of(a, r, blockIdx.x == 0);
-    uint64_t n = (uint64_t)x.tiles * x.parts;
+    if (r < a.n_requests) x = request_of(a, r, blockIdx.x == 0 && threadIdx.x < 64);
+    mine[lane_id()] = x;
+    n = x.tiles * x.parts;
+    sum = n;
     for (int i = 1; i < 64; i <<= 1) {
-      const uint64_t y = __shfl_up(n, i);
-      if (lane >= i) n += y;
+      const uint32_t y = __shfl_up(sum, i);
+      if (lane_id() >= i) sum += y;
     }
-    __syncthreads();  // the readers of the requests before are done
-    if (lane == 63) s->sums[wave] = n;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) n += s->sums[i];
-    s->pre[threadIdx.x + 1] = n;
-    if (threadIdx.x == 0) s->pre[0] = 0;
-    s->req[threadIdx.x] = x;
-    __syncthreads();
+    all = __builtin_amdgcn_readlane(sum, 63);
   }
 
   // Item `at` (ascending from call to call); false behind the last one.  A
   // request's last tiles come first: later rows see more.
-  __device__ __forceinline__ bool find(const AttendArgs &a, Items *s, uint64_t at, Item *it) {
+  __device__ __forceinline__ bool find(const AttendArgs &a, uint64_t at, Item *it) {
     const uint64_t item = at / a.c.n_heads;
     it->h = (uint32_t)(at - item * a.c.n_heads);
-    while (item - base >= s->pre[kAttThreads]) {
-      base += s->pre[kAttThreads];
-      r0 += kAttThreads;
+    while (item - base >= all) {
+      base += all;
+      r0 += 64;
       if (r0 >= a.n_requests) return false;
-      scan(a, s);
+      scan(a);
     }
-    uint32_t i = 0;
-#pragma unroll
-    for (int k = kAttThreads / 2; k; k >>= 1)
-      if (s->pre[i + k] <= item - base) i += k;
-    i = __builtin_amdgcn_readfirstlane(i);
+    const uint32_t j = (uint32_t)(item - base);
+    const uint32_t i = (uint32_t)__popcll(__ballot(sum <= j));
+    const uint32_t k = j - (__builtin_amdgcn_readlane(sum, i) - __builtin_amdgcn_readlane(n, i));
     it->r = r0 + i;
-    it->x = uniform(s->req[i]);
-    const uint32_t k = __builtin_amdgcn_readfirstlane((uint32_t)(item - base - s->pre[i]));
+    it->x = uniform(mine[i]);
     it->tile = it->x.tiles - 1 - k / it->x.parts;
     it->part = it->x.part0 + k % it->x.parts;
     return true;
@@ -474,12 +462,13 @@ constexpr int resident(int d, int nq) {
 template <int DT, int FMT, int D, int NQ>
 __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendArgs a) {
   __shared__ Parked<D, NQ> parked[2];
-  __shared__ Items items;
+  __shared__ Request requests[kAttThreads];
   const int wave = threadIdx.x >> 6, lane = lane_id();
   ItemWalk walk;
-  walk.scan(a, &items);
+  walk.mine = requests + 64 * wave;
+  walk.scan(a);
   Item it;
-  for (uint64_t at = blockIdx.x; walk.find(a, &items, at, &it); at += gridDim.x) {
+  for (uint64_t at = blockIdx.x; walk.find(a, at, &it); at += gridDim.x) {
     const Request &x = it.x;
     const Tile t = tile_of(a, x, it.tile);
     const bool none = t.part0 == t.part1;  // no row sees anything: the first item says so
@@ -534,49 +523,28 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   return r;
 }
 
-// The item of a workgroup: part and tile (a request's last tiles, which see
-// most, first) of a request, and a head.  A wave counts the items 64 requests
-// at a time, so that the workgroups with work are side by side and spread
-// evenly over the CUs; above 512 requests that would take longer than the
-// work, and an item's place alone says whose it is (some then have none).
-__device__ __forceinline__ bool find_item(const AttendArgs &a, uint32_t at, Item *it) {
+// The item of a workgroup.  Above 512 requests counting would take longer than
+// the work, and an item's place alone says whose it is; some workgroups then
+// have none (with few requests that would leave CUs idle: the ones with work
+// would not be spread evenly).
+__device__ __forceinline__ bool find_item(const AttendArgs &a, Request *mine, uint32_t at,
+                                          Item *it) {
+  if (a.n_requests <= 512) {
+    ItemWalk walk;
+    walk.mine = mine;
+    walk.scan(a);
+    return walk.find(a, at, it);
+  }
   const uint32_t item = at / a.c.n_heads;
   it->h = at - item * a.c.n_heads;
-  uint32_t k = 0;
-  if (a.n_requests > 512) {
-    const Places pl = {a.q_start, a.n_requests, a.group, a.plan.rows, 1u};
-    const uint32_t place = item / a.plan.splits;
-    it->r = __builtin_amdgcn_readfirstlane(pl.find(place));
-    it->x = uniform(request_of(a, it->r, threadIdx.x == 0));
-    const uint32_t tile = place - __builtin_amdgcn_readfirstlane((uint32_t)pl.first(it->r));
-    k = tile * it->x.parts + item % a.plan.splits;
-    if (tile >= it->x.tiles || item % a.plan.splits >= it->x.parts) return false;
-  } else {
-    uint32_t base = 0;
-    for (uint32_t r0 = 0;; r0 += 64) {
-      if (r0 >= a.n_requests) return false;
-      const uint32_t r = r0 + lane_id();
-      Request x = {};
-      if (r < a.n_requests) x = request_of(a, r, threadIdx.x < 64 && at == 0);
-      const uint32_t n = x.tiles * x.parts;
-      uint32_t sum = n;
-      for (int i = 1; i < 64; i <<= 1) {
-        const uint32_t y = __shfl_up(sum, i);
-        if (lane_id() >= i) sum += y;
-      }
-      const uint32_t all = __builtin_amdgcn_readlane(sum, 63);
-      if (item - base < all) {
-        const uint32_t i = (uint32_t)__popcll(__ballot(sum <= item - base));
-        it->r = r0 + i;
-        it->x = from_lane(x, i);
-        k = item - base - (__builtin_amdgcn_readlane(sum, i) - __builtin_amdgcn_readlane(n, i));
-        break;
-      }
-      base += all;
-    }
-  }
-  it->tile = it->x.tiles - 1 - k / it->x.parts;
-  it->part = it->x.part0 + k % it->x.parts;
+  const Places pl = {a.q_start, a.n_requests, a.group, a.plan.rows, 1u};
+  const uint32_t place = item / a.plan.splits, nth = item % a.plan.splits;
+  it->r = __builtin_amdgcn_readfirstlane(pl.find(place));
+  it->x = uniform(request_of(a, it->r, threadIdx.x == 0));
+  const uint32_t tile = place - __builtin_amdgcn_readfirstlane((uint32_t)pl.first(it->r));
+  if (tile >= it->x.tiles || nth >= it->x.parts) return false;
+  it->tile = it->x.tiles - 1 - tile;
+  it->part = it->x.part0 + nth;
   return true;
 }
 
@@ -607,8 +575,9 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   const int c16 = lane & 15, g = lane >> 4, ka = c16 >> 2, kb = c16 & 3;
   const uint32_t bt = 1u << a.bt_log2;
+  __shared__ Request requests[64 * kWaves];
   Item it;
-  if (!find_item(a, blockIdx.x, &it)) return;
+  if (!find_item(a, requests + 64 * wave, blockIdx.x, &it)) return;
   const Request &x = it.x;
   const Tile t = tile_of(a, x, it.tile);
   const bool none = t.part0 == t.part1;

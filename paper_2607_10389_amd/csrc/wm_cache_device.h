@@ -177,20 +177,6 @@ __device__ __forceinline__ uint64_t part_place(const AttendArgs &a, const Reques
   return ((place * a.plan.splits + part) * a.c.n_heads + h) * a.plan.rows;
 }
 
-// Lane i's request, for the whole wave.
-__device__ __forceinline__ Request from_lane(const Request &x, uint32_t i) {
-  Request y = x;
-  y.q0 = (int64_t)__builtin_amdgcn_readlane((int)x.q0, i);
-  y.n_rows = __builtin_amdgcn_readlane(x.n_rows, i);
-  y.tiles = __builtin_amdgcn_readlane(x.tiles, i);
-  y.len = __builtin_amdgcn_readlane(x.len, i);
-  y.pos0 = __builtin_amdgcn_readlane(x.pos0, i);
-  y.cut = __builtin_amdgcn_readlane(x.cut, i);
-  y.part0 = __builtin_amdgcn_readlane(x.part0, i);
-  y.parts = __builtin_amdgcn_readlane(x.parts, i);
-  return y;
-}
-
 // The same request in every lane of a wave, told to the compiler.
 __device__ __forceinline__ Request uniform(const Request &x) {
   Request y = x;
