@@ -77,30 +77,31 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, const Request 
   }
 }
 
-// A wave's rows into the output, or into the workspace if the tile has several
-// parts.  place: the workspace's place of row0.
+// A wave's rows into the output, or as part `part` into the workspace if the
+// tile has several.
 template <int DT, int FMT, int D, int NQ>
 __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x, uint32_t row0,
                                            uint32_t h, const Rows<D, NQ> &w, float lift,
-                                           bool whole, uint64_t place) {
+                                           bool whole, uint32_t part) {
   const int lane = lane_id(), c16 = lane & 15, g = lane >> 4;
   const bool wide = (((uintptr_t)a.out.ptr >> 1 | a.out.row_stride | a.out.head_stride) & 3u) == 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const uint32_t row = row0 + 16 * n + c16;
     if (row >= x.n_rows) continue;
+    const uint64_t tok = (uint64_t)x.q0 + row / a.group;
+    const uint32_t hq = h * a.group + row % a.group;
     const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? w.vref / w.l[n] : 0.0f;
     const float lse2 = w.l[n] == 0.0f ? kNegInf : w.m[n] + __builtin_amdgcn_logf(w.l[n]) - lift;
     if (!whole) {
-      const uint64_t to = place + 16 * n + c16;
+      const uint64_t to = part_place(a, tok, hq) + part;
       float *po = a.part_out + to * D + 4 * g;
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) *(f32x4 *)(po + 16 * j) = w.o[n][j] * inv;
       if (g == 0) a.part_lse[to] = lse2;
       continue;
     }
-    const uint32_t tok = row / a.group, hq = h * a.group + row % a.group;
-    uint16_t *op = (uint16_t *)a.out.ptr + (uint64_t)(x.q0 + tok) * a.out.row_stride +
+    uint16_t *op = (uint16_t *)a.out.ptr + tok * a.out.row_stride +
                    (uint64_t)hq * a.out.head_stride + 4 * g;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
@@ -116,7 +117,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x
       }
     }
     if (g == 0 && a.lse)
-      a.lse[(uint64_t)(x.q0 + tok) * (a.group * a.c.n_heads) + hq] = lse2 * 0.6931471805599453f;
+      a.lse[tok * (a.group * a.c.n_heads) + hq] = lse2 * 0.6931471805599453f;
   }
 }
 
@@ -162,6 +163,7 @@ struct ItemWalk {
     }
     const uint32_t j = (uint32_t)(item - base);
     const uint32_t i = (uint32_t)__popcll(__ballot(sum <= j));
+    if (i > 63) return false;  // starts that do not ascend
     const uint32_t k = j - (__builtin_amdgcn_readlane(sum, i) - __builtin_amdgcn_readlane(n, i));
     it->r = r0 + i;
     it->x = uniform(mine[i]);
@@ -490,9 +492,7 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
     if (wave) continue;
     join(&w, parked[0], lane);
     const bool whole = t.part1 - t.part0 <= 1;
-    store_rows<DT, FMT, D, NQ>(
-        a, x, t.row0, it.h, w, kLift, whole,
-        whole ? 0 : part_place(a, x, it.r, it.tile, it.part - t.part0, it.h));
+    store_rows<DT, FMT, D, NQ>(a, x, t.row0, it.h, w, kLift, whole, it.part - t.part0);
   }
 }
 
@@ -844,9 +844,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   }
   if (idle) return;
   const bool whole = t.part1 - t.part0 <= 1;
-  store_rows<DT, FMT, D, NQ>(
-      a, x, row0, h, w, kLiftMany, whole,
-      whole ? 0 : part_place(a, x, it.r, it.tile, it.part - t.part0, h) + wave * 16 * NQ);
+  store_rows<DT, FMT, D, NQ>(a, x, row0, h, w, kLiftMany, whole, it.part - t.part0);
 }
 
 template <int DT, int FMT, int D>

@@ -208,7 +208,7 @@ uint64_t wm_attend_ws_bytes(uint32_t n_requests, uint32_t n_tokens, uint32_t n_h
                             uint32_t n_q_heads, uint32_t head_dim, uint32_t max_len) {
   const AttendPlan p = attend_plan(n_requests, n_tokens, n_heads, n_q_heads, head_dim, max_len);
   if (p.splits <= 1) return 0;
-  return (uint64_t)p.tiles * n_heads * p.splits * p.rows * (head_dim + 1u) * 4u;
+  return (uint64_t)n_tokens * n_q_heads * p.splits * (head_dim + 1u) * 4u;
 }
 
 wm_status wm_cache_attend(const wm_cache *cache, const wm_rows *q, const wm_rows *out, float *lse,
@@ -233,7 +233,7 @@ wm_status wm_cache_attend(const wm_cache *cache, const wm_rows *q, const wm_rows
       !aligned(block_table, 4) || !aligned(len, 4) || !aligned(q_start, 4))
     return WM_ERR_INVALID_ARG;
   a.plan = attend_plan(n_requests, n_tokens, cache->n_heads, n_q_heads, cache->head_dim, max_len);
-  const uint64_t vectors = (uint64_t)a.plan.tiles * cache->n_heads * a.plan.splits * a.plan.rows;
+  const uint64_t vectors = (uint64_t)n_tokens * n_q_heads * a.plan.splits;
   a.part_out = a.part_lse = nullptr;
   if (a.plan.splits > 1) {
     if (!ws || !aligned(ws, 16) || ws_bytes < vectors * (cache->head_dim + 1u) * 4u)

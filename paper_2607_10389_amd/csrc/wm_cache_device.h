@@ -170,11 +170,10 @@ __device__ __forceinline__ Tile tile_of(const AttendArgs &a, const Request &x, u
   return t;
 }
 
-// Where a tile's parts lie in the workspace.
-__device__ __forceinline__ uint64_t part_place(const AttendArgs &a, const Request &x, uint32_t r,
-                                               uint32_t tile, uint32_t part, uint32_t h) {
-  const uint64_t place = (uint64_t)x.q0 * a.group / a.plan.rows + r + tile;
-  return ((place * a.plan.splits + part) * a.c.n_heads + h) * a.plan.rows;
+// Where a row's parts lie in the workspace: side by side, so that joining them
+// reads one stretch.
+__device__ __forceinline__ uint64_t part_place(const AttendArgs &a, uint64_t token, uint32_t hq) {
+  return (token * (a.group * a.c.n_heads) + hq) * a.plan.splits;
 }
 
 // The same request in every lane of a wave, told to the compiler.

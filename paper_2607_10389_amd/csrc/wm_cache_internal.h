@@ -50,7 +50,7 @@ struct AttendArgs {
   uint64_t table_stride;
   const int32_t *len, *q_start;
   uint32_t *verdict;
-  float *part_out, *part_lse;  // workspace: [tiles][splits][heads][rows] vectors, numbers
+  float *part_out, *part_lse;  // workspace: [tokens][query heads][splits] vectors, numbers
   AttendPlan plan;
   uint32_t n_requests, n_tokens, group, max_blocks, bt_log2, window, n_cu;
   float scale_log2;  // scale * log2(e)

@@ -412,21 +412,20 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
   const uint64_t at = (uint64_t)blockIdx.x * (kAttThreads / 64) + (threadIdx.x >> 6);
   const uint64_t token = at / hq_all;
   if (token >= a.n_tokens) return;
-  const uint32_t hq = (uint32_t)(at - token * hq_all), h = hq / a.group;
+  const uint32_t hq = (uint32_t)(at - token * hq_all);
   const Places pl = {a.q_start, a.n_requests, 1u, 1u, 0u};
   const uint32_t r = __builtin_amdgcn_readfirstlane(pl.find((int64_t)token));
   const Request x = request_of(a, r, false);
   if ((int64_t)token < x.q0) return;
-  const uint64_t row = (token - (uint64_t)x.q0) * a.group + (hq - h * a.group);
+  const uint64_t row = (token - (uint64_t)x.q0) * a.group + hq % a.group;
   if (row >= x.n_rows) return;
   const uint32_t tile = (uint32_t)row / a.plan.rows;
   const Tile t = tile_of(a, x, tile);
   const uint32_t n = t.part1 - t.part0;
   if (n <= 1) return;
   const int lane = lane_id();
-  const uint64_t p0 = part_place(a, x, r, tile, 0, h) + row % a.plan.rows;
-  const uint64_t step = (uint64_t)a.c.n_heads * a.plan.rows;  // from a part to the next
-  const float z = (uint32_t)lane < n ? a.part_lse[p0 + lane * step] : kNegInf;
+  const uint64_t p0 = part_place(a, token, hq);
+  const float z = (uint32_t)lane < n ? a.part_lse[p0 + lane] : kNegInf;
   float top = z;
   for (int i = 32; i; i >>= 1) top = fmaxf(top, __shfl_xor(top, i));
   const float use = top == kNegInf ? 0.0f : top;
@@ -444,7 +443,7 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
     for (int k = 0; k < 8; ++k) {
       const uint32_t kk = k0 + k < n ? k0 + k : n - 1;
 #pragma unroll
-      for (int j = 0; j < KD; ++j) y[k][j] = p[kk * step * (64 * KD) + j];
+      for (int j = 0; j < KD; ++j) y[k][j] = p[(uint64_t)kk * (64 * KD) + j];
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {

@@ -648,3 +648,136 @@ def test_captured_step_replays(wm):
         lens.copy_(nxt)
         nxt.add_(1)
         pi.copy_(po)
+
+
+# ---- ranges ------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("fmt", [E4, E5])
+def test_prompts_of_every_size_and_type(wm, dim, dt, fmt):
+    """Tiles with steps that every row sees whole, with masked ones, and with
+    both ends of a window."""
+    bt = {64: 16, 128: 64, 192: 32, 256: 128}[dim]
+    check_attend(wm, [300, 77], [40, 60], 1, 4, bt, dim, dt, fmt, seed=dim)
+    check_attend(wm, [400], [70], 1, 3, bt, dim, dt, fmt, seed=dim + 1, window=150)
+
+
+@pytest.mark.parametrize("lens,new,heads,group,dim,more", [
+    # rows without anything to see among prompts
+    ([0, 20, 200], [40, 50, 40], 1, 2, 64, {}),
+    # few tiles over long sequences: parts, joined
+    ([5000], [40], 1, 2, 64, {}),
+    ([2600, 70, 0], [33, 33, 40], 1, 1, 128, dict(window=1100)),
+    ([4000, 900], [50, 45], 2, 1, 256, dict(max_len=1000)),
+    # a mix of a prompt and single tokens
+    ([130, 500, 64, 1], [100, 1, 1, 1], 2, 4, 64, {})])
+def test_prompts_at_the_edges(wm, lens, new, heads, group, dim, more):
+    check_attend(wm, lens, new, heads, group, 32, dim, BF, E4, **more)
+
+
+def test_many_requests(wm):
+    """More requests than a wave counts at once: single tokens of 300, short
+    prompts of 150 and of 600 (whose items are found by their place)."""
+    g = np.random.default_rng(1)
+    check_attend(wm, g.integers(0, 700, 300).tolist(), [1] * 300, 1, 2, 16, 64, BF, E4)
+    for n in (150, 600):
+        new = g.integers(0, 20, n)
+        lens = new + g.integers(0, 40, n)
+        check_attend(wm, lens.tolist(), new.tolist(), 1, 5, 16, 64, BF, E4)
+
+
+def test_a_token_is_answered_the_same_in_any_batch(wm):
+    bt, heads, group, dim = 16, 2, 4, 128
+    lens = [1900, 3, 5000, 700]
+    rows, blocks = layout(lens, bt, 21)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, E4, 22)
+    q = torch.randn(4, heads * group, dim).to(BF).cuda()
+
+    def ask(ids, most):
+        out = torch.zeros(len(ids), heads * group, dim, dtype=BF, device="cuda")
+        ln = dev([lens[i] for i in ids])
+        ws = torch.empty(wm.attend_ws_bytes(out, k, ln, most), dtype=torch.uint8, device="cuda")
+        wm.cache_attend(q[ids].contiguous(), k, v, ks, vs, dev([rows[i] for i in ids]), ln,
+                        dev(list(range(len(ids) + 1))), out, ws, max_len=most, scale=0.09)
+        return out
+    every = ask([0, 1, 2, 3], 5000)
+    for i in range(4):
+        assert torch.equal(ask([i], lens[i])[0], every[i]), i
+        assert torch.equal(ask([3, i], 100_000)[1], every[i]), i
+
+
+def far_pool(blocks, page, step=1 << 30):
+    """Pages a GiB apart: offsets beyond 32 bits with few blocks."""
+    buf = torch.empty((blocks - 1) * step + page, dtype=torch.uint8, device="cuda")
+    return buf.as_strided((blocks, page), (step, 1))
+
+
+def test_offsets_beyond_32_bits(wm):
+    heads, bt, dim, blocks = 1, 16, 64, 6
+    page = heads * bt * dim
+    near = make_cache(blocks, heads, bt, dim, E4, 31)
+    far_k, far_v = far_pool(blocks, page), far_pool(blocks, page)
+    k = far_k.view(E4).view(blocks, heads, bt, dim)
+    v = far_v.view(E4).view(blocks, heads, dim, bt)
+    k.view(torch.uint8).copy_(near[0].view(torch.uint8))
+    v.view(torch.uint8).copy_(near[1].view(torch.uint8))
+    far = [k, v, near[2].clone(), near[3].clone()]
+    rows, lens = [[5, 4], [3, 0]], [20, 32]
+    x = torch.randn(4, heads, dim).to(BF).cuda()
+    slots = dev([5 * 16 + 15, 4 * 16, 4 * 16 + 1, 0], torch.int64)
+    q, outs = torch.randn(2, 2, dim).to(BF).cuda(), []
+    for c in (near, far):
+        verdict = word()
+        wm.cache_append(x, x, *c, slots, dev([0, 3, 4]), verdict)
+        out = torch.zeros_like(q)
+        wm.cache_attend(q, *c, dev(rows), dev(lens), dev([0, 1, 2]), out, max_len=32, scale=0.1,
+                        verdict=verdict)
+        assert verdict.item() == 0
+        outs.append(out)
+    assert torch.equal(*outs) and bool(outs[0].any())
+    assert torch.equal(far[0].view(torch.uint8), near[0].view(torch.uint8))
+    assert torch.equal(far[1].view(torch.uint8), near[1].view(torch.uint8))
+    flat, verdict = torch.zeros(3 * page, dtype=torch.uint8, device="cuda"), word()
+    wm.flatten_pages([far_k], dev([5, 1, 4]), flat, verdict)
+    assert torch.equal(flat.view(3, page), far_k[[5, 1, 4]])
+    wm.rehydrate_pages(flat, [far_v], dev([4, 0, 5]), verdict)
+    assert torch.equal(far_v[[4, 0, 5]], flat.view(3, page)) and verdict.item() == 0
+
+
+def test_blocks_without_a_usable_scale_count_as_fresh(wm):
+    for bad in (0.0, -1.0, math.nan, math.inf, 1e-42):
+        k, v, ks, vs = make_cache(2, 1, 16, 64, E4, 41)
+        ks[1, 0] = vs[1, 0] = bad
+        x = torch.randn(2, 1, 64).to(BF).cuda()
+        wm.cache_append(x, x, k, v, ks, vs, dev([21, 22], torch.int64), dev([0, 2]))
+        want, scale = ref.append(x.cpu(), torch.zeros_like(k.cpu().view(torch.uint8)).view(E4),
+                                 torch.ones(2, 1), [16, 17], [0, 2], False)
+        assert ks[1, 0].item() == scale[1, 0].item() == vs[1, 0].item()
+        got = ref.decode(k.cpu())[1, 0]
+        assert torch.equal(got[5:7], want[1, 0, :2]) and not got[:5].any() and not got[7:].any()
+        got = ref.decode(v.cpu())[1, 0].t()
+        assert torch.equal(got[5:7], want[1, 0, :2]) and not got[:5].any() and not got[7:].any()
+
+
+def test_calls_on_two_streams_at_once(wm):
+    bt, lens = 64, [3000, 2500]
+    rows, blocks = layout(lens, bt, 51)
+    k, v, ks, vs = make_cache(blocks, 2, bt, 128, E4, 52)
+    args = (k, v, ks, vs, dev(rows), dev(lens), dev([0, 1, 2]))
+    qs = [torch.randn(2, 8, 128).to(BF).cuda() for _ in range(2)]
+    n = wm.attend_ws_bytes(qs[0], k, dev(lens), 3000)
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    want = []
+    for q in qs:
+        want.append(torch.zeros_like(q))
+        wm.cache_attend(q, *args, want[-1], ws[0], max_len=3000, scale=0.1)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for q, o, w, s in zip(qs, outs, ws, streams):
+            wm.cache_attend(q, *args, o, w, max_len=3000, scale=0.1, stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
