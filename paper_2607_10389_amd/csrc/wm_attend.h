@@ -612,15 +612,17 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   if (s0 < s_part) s0 = s_part;
   if (s1 > s_part + (1u << (x.cut - 6))) s1 = s_part + (1u << (x.cut - 6));
 
-  const uint8_t *kbase = (const uint8_t *)a.c.k + ((uint64_t)h * bt + kb + 4 * (wave & 3)) * D +
-                         (wave >> 2) * 64 + g * 16;
-  const uint8_t *vbase = (const uint8_t *)a.c.v + ((uint64_t)h * D + 16 * wave + c16) * bt;
+  // the lane's place in a step's keys and values
+  const uint32_t k_lane = (kb + 4 * (wave & 3)) * D + (wave >> 2) * 64 + g * 16;
+  const uint32_t v_lane = (16 * wave + c16) * bt;
   const int32_t *row = a.table + (uint64_t)it.r * a.table_stride;
   bool bad_page = false;
-  // the table's entry for token j (a multiple of 16), and the block that it is:
+  // the table's entry for the n tokens from j on (in one block), and the block that it is:
   // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
   // when it is needed: looking at once would wait for it.)
-  auto entry_of = [&](uint32_t j) { return row[(j < t.hi && j + 16 > t.lo ? j : t.lo) >> a.bt_log2]; };
+  auto entry_of = [&](uint32_t j, uint32_t n) {
+    return row[(j < t.hi && j + n > t.lo ? j : t.lo) >> a.bt_log2];
+  };
   auto block_of = [&](int32_t id, uint32_t j) -> int32_t {
     const bool in = j < t.hi && j + 16 > t.lo, out = in && (uint32_t)id >= a.c.n_blocks;
     bad_page |= out;
@@ -634,23 +636,42 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   int32_t idk1 = -1, idv1 = -1;  // blocks of the step that is loaded
   int32_t ek = 0, ev = 0;        // entries of the one after
   auto blocks = [&](uint32_t s) {
-    ek = entry_of((s << 6) + 16 * ka);
-    ev = entry_of((s << 6) + 16 * g);
+    if (a.bt_log2 >= 6) {
+      ev = entry_of(s << 6, 64);
+    } else {
+      ek = entry_of((s << 6) + 16 * ka, 16);
+      ev = entry_of((s << 6) + 16 * g, 16);
+    }
+  };
+  auto load_from = [&](const uint8_t *kp, uint32_t k_off, const uint8_t *vp, uint32_t v_off) {
+#pragma unroll
+    for (int j = 0; j < KW; ++j)
+      if (has_k(j)) kg[j] = *(const u32x4 *)(kp + (k_off + j * KS * 64));
+#pragma unroll
+    for (int j = 0; j < VW; ++j)
+      if (has_v(j)) vg[j] = *(const u32x4 *)(vp + (uint64_t)j * kWaves * 16 * bt + v_off);
   };
   auto load = [&](uint32_t s) {
     const uint32_t t0 = s << 6;
-    idk1 = block_of(ek, t0 + 16 * ka);
-    idv1 = block_of(ev, t0 + 16 * g);
-    const uint8_t *kp = kbase + (uint64_t)(idk1 < 0 ? 0 : idk1) * a.c.k_stride +
-                        ((t0 + 16 * ka) & (bt - 1)) * D;
-    const uint8_t *vp = vbase + (uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_stride +
-                        ((t0 + 16 * g) & (bt - 1));
-#pragma unroll
-    for (int j = 0; j < KW; ++j)
-      if (has_k(j)) kg[j] = *(const u32x4 *)(kp + j * KS * 64);
-#pragma unroll
-    for (int j = 0; j < VW; ++j)
-      if (has_v(j)) vg[j] = *(const u32x4 *)(vp + (uint64_t)j * kWaves * 16 * bt);
+    const uint8_t *kh = (const uint8_t *)a.c.k + (uint64_t)h * bt * D;
+    const uint8_t *vh = (const uint8_t *)a.c.v + (uint64_t)h * bt * D;
+    if (a.bt_log2 >= 6) {
+      // a step lies in one block: one address for the wave, and 32-bit places
+      const int32_t id = __builtin_amdgcn_readfirstlane(ev);
+      const bool out = (uint32_t)id >= a.c.n_blocks;
+      bad_page |= out;
+      idk1 = idv1 = out ? -1 : id;
+      const uint64_t at = out ? 0u : (uint64_t)id;
+      load_from(kh + at * a.c.k_stride + (t0 & (bt - 1)) * D, k_lane + 16 * ka * D,
+                vh + at * a.c.v_stride + (t0 & (bt - 1)), v_lane + 16 * g);
+    } else {
+      idk1 = block_of(ek, t0 + 16 * ka);
+      idv1 = block_of(ev, t0 + 16 * g);
+      load_from(kh + (uint64_t)(idk1 < 0 ? 0 : idk1) * a.c.k_stride +
+                    ((t0 + 16 * ka) & (bt - 1)) * D, k_lane,
+                vh + (uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_stride + ((t0 + 16 * g) & (bt - 1)),
+                v_lane);
+    }
     ks1 = a.c.k_scale[(uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.k_scale_stride + h];
     vs1 = a.c.v_scale[(uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_scale_stride + h];
   };

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -48,11 +49,15 @@ bool check_rows(const wm_rows *r) {
   return r && !r->flags && (r->dtype == WM_BF16 || r->dtype == WM_FP16) && aligned(r->ptr, 2);
 }
 
+// CUs of the current device (0: none); asked of the runtime once per device.
 int cus() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 0;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
     return 0;
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
