@@ -10,6 +10,7 @@ namespace {
 // precision: at most 2^15 then, and a weight of 2^-29 of the largest still has
 // all its bits (2^-40 its last one)
 constexpr float kLift = 15.0f;
+constexpr float kUnitLow = 0x1p-64f;  // see unit_of()
 
 // What a wave holds of its 16 NQ rows.  A lane has one row of each 16 (column
 // lane % 16 of the matrix core's result) and of the output the dimensions
@@ -19,6 +20,7 @@ struct Rows {
   f32x4 o[NQ][D / 16];
   float m[NQ], l[NQ];  // maximum of the scores (base 2) and sum of the weights
   float vref;          // o is in units of vref 2^-kLift
+  float vtop;          // the largest scale of the values so far
 };
 
 template <int D, int NQ>
@@ -31,6 +33,18 @@ __device__ __forceinline__ void clear(Rows<D, NQ> *w) {
     for (int j = 0; j < D / 16; ++j) w->o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   w->vref = 0x1p-125f;  // below it a scale has no exact reciprocal
+  w->vtop = 0x1p-125f / kUnitLow;
+}
+
+// The unit of the value sums in a step whose largest scale is `most`: the
+// largest scale so far, as a rule.  Weights are rounded to half precision in
+// that unit, so where a step's scales are over 2^6 below it, the unit comes
+// down to them, by 2^64 from the largest at most: the sums, up to 2^57 units
+// over 2^26 tokens, cannot overflow.
+__device__ __forceinline__ float unit_of(float unit, float most, float *top) {
+  *top = fmaxf(*top, most);
+  const bool low = most > 0.0f && most < unit * 0x1p-6f;
+  return fmaxf(low ? *top * kUnitLow : unit, most);
 }
 
 // The maximum over the four lane groups that share a row.
@@ -133,13 +147,14 @@ struct Item {
 
 struct ItemWalk {
   Request *mine;        // LDS: the wave's 64 requests
+  bool tell;            // say so of lengths beyond the table
   uint64_t base = 0;    // items before them
   uint32_t r0 = 0, n = 0, sum = 0, all = 0;  // a lane's items, with those before it, all 64's
 
   __device__ __forceinline__ void scan(const AttendArgs &a) {
     const uint32_t r = r0 + lane_id();
     Request x = {};
-    if (r < a.n_requests) x = request_of(a, r, blockIdx.x == 0 && threadIdx.x < 64);
+    if (r < a.n_requests) x = request_of(a, r, tell);
     mine[lane_id()] = x;
     n = x.tiles * x.parts;
     sum = n;
@@ -236,7 +251,9 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
   // the table's entry for token j (a multiple of 16), and the block that it is:
   // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
   // when it is needed: looking at once would wait for it.)
-  auto entry_of = [&](uint32_t j) { return row[(j < t.hi && j + 16 > t.lo ? j : t.lo) >> a.bt_log2]; };
+  auto entry_of = [&](uint32_t j) {
+    return row[(j < t.hi && j + 16 > t.lo ? j : t.lo) >> a.bt_log2];
+  };
   auto block_of = [&](int32_t id, uint32_t j) -> int32_t {
     const bool in = j < t.hi && j + 16 > t.lo, out = in && (uint32_t)id >= a.c.n_blocks;
     bad_page |= out;
@@ -331,9 +348,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
           if (i > end || i <= begin) sc[n][i >> 2][i & 3] = kNegInf;
       }
     }
-    // the values' unit: the largest scale so far
-    const float vmax = group_max(fabsf(vs));
-    const float vref = fmaxf(w->vref, vmax);
+    const float vref = unit_of(w->vref, group_max(vs), &w->vtop);
     const float vscale = vs / vref, shrink = w->vref / vref;
     w->vref = vref;
     f16x8 p[NQ][2], p_low[NQ][2];
@@ -468,6 +483,7 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
   const int wave = threadIdx.x >> 6, lane = lane_id();
   ItemWalk walk;
   walk.mine = requests + 64 * wave;
+  walk.tell = blockIdx.x == 0 && wave == 0;  // it goes through all requests
   walk.scan(a);
   Item it;
   for (uint64_t at = blockIdx.x; walk.find(a, at, &it); at += gridDim.x) {
@@ -500,9 +516,16 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 //
 // Prompts: a tile of 128 rows, 16 NQ of them per wave, and every wave goes
 // through all of the tile's steps.  A step's keys and values are converted
-// once for all waves, each a share, and lie in LDS as the matrix instructions' left operands, 16 bytes
-// a lane in lane order: reads and writes without bank conflicts.  Two steps'
-// worth, so one barrier a step.
+// once for all waves, each a share, and lie in LDS as the matrix instructions'
+// left operands, 16 bytes a lane in lane order: reads and writes without bank
+// conflicts.  Two steps' worth, so one barrier a step.
+//
+// Up to 128 dimensions four waves have two row blocks each.  Two leave room
+// for a second wave on the SIMD, whose products run beside this one's
+// exponentials (three or four blocks read LDS less often, but were slower:
+// 288 and 524 us where two took 256).  192 dimensions and more: eight waves
+// with a block each, so that the sums still fit into 256 registers; the tile
+// is 128 rows either way.
 //
 // What bounds it is the vector ALU beside the matrix cores (half a maximum, an
 // exponential, two fused products and a rounding per score), so little else
@@ -513,9 +536,8 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // run in a loop without masks.
 constexpr float kSlack = 4.0f, kLiftMany = 11.0f;
 
-// Row blocks of a wave.  Two leave room for a second wave on the SIMD, whose
-// products run beside this one's exponentials (three or four blocks read LDS
-// less often, but were slower: 288 and 524 us where two take 256).
+constexpr int many_waves(int d) { return d <= 128 ? 4 : 8; }
+
 // (Written out: fmaxf would first turn each operand's signalling NaN quiet.)
 __device__ __forceinline__ float max3(float x, float y, float z) {
   float r;
@@ -532,6 +554,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs &a, Request *mine, ui
   if (a.n_requests <= 512) {
     ItemWalk walk;
     walk.mine = mine;
+    walk.tell = false;
     walk.scan(a);
     return walk.find(a, at, it);
   }
@@ -540,7 +563,7 @@ __device__ __forceinline__ bool find_item(const AttendArgs &a, Request *mine, ui
   const Places pl = {a.q_start, a.n_requests, a.group, a.plan.rows, 1u};
   const uint32_t place = item / a.plan.splits, nth = item % a.plan.splits;
   it->r = __builtin_amdgcn_readfirstlane(pl.find(place));
-  it->x = uniform(request_of(a, it->r, threadIdx.x == 0));
+  it->x = uniform(request_of(a, it->r, false));
   const uint32_t tile = place - __builtin_amdgcn_readfirstlane((uint32_t)pl.first(it->r));
   if (tile >= it->x.tiles || nth >= it->x.parts) return false;
   it->tile = it->x.tiles - 1 - tile;
@@ -554,11 +577,6 @@ struct Yes {
 struct No {
   static constexpr bool value = false;
 };
-
-//
-// 192 dimensions and more: twice the waves with a block each, so that the sums
-// still fit into 256 registers; the tile is 128 rows either way.
-constexpr int many_waves(int d) { return d <= 128 ? 4 : 8; }
 
 template <int DT, int FMT, int D>
 __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArgs a) {
@@ -578,6 +596,9 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   __shared__ Request requests[64 * kWaves];
   Item it;
   if (!find_item(a, requests + 64 * wave, blockIdx.x, &it)) return;
+  // (every request with new tokens has an item, whose workgroup speaks for it)
+  if (threadIdx.x == 0 && a.verdict && (int64_t)a.len[it.r] > (int64_t)a.max_blocks << a.bt_log2)
+    atomicOr(a.verdict, WM_C_LENGTH);
   const Request &x = it.x;
   const Tile t = tile_of(a, x, it.tile);
   const bool none = t.part0 == t.part1;
@@ -617,9 +638,9 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const uint32_t v_lane = (16 * wave + c16) * bt;
   const int32_t *row = a.table + (uint64_t)it.r * a.table_stride;
   bool bad_page = false;
-  // the table's entry for the n tokens from j on (in one block), and the block that it is:
-  // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
-  // when it is needed: looking at once would wait for it.)
+  // the table's entry for the n tokens from j on, which lie in one block, and
+  // the block that it is: -1 if no row sees its 16 tokens.  (The entry is
+  // looked at a step later, when it is needed: looking at once would wait.)
   auto entry_of = [&](uint32_t j, uint32_t n) {
     return row[(j < t.hi && j + n > t.lo ? j : t.lo) >> a.bt_log2];
   };
@@ -716,8 +737,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       load(s + 1);
       blocks(s + 2);
     }
-    // the values' unit is the largest scale so far
-    vref = fmaxf(vref, group_max(vs));
+    vref = unit_of(vref, group_max(vs), &w.vtop);
     const float ratio = fmaxf(vs * __builtin_amdgcn_rcpf(vref), 0x1p-60f);
     __syncthreads();
     const int t0 = (int)(s << 6);
@@ -795,7 +815,8 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
         for (int i = 0; i < VT; ++i) w.o[n][i] *= keep * shrink;
       }
     }
-    const float back = __builtin_amdgcn_rcpf(ratio), lift = kLiftMany + __builtin_amdgcn_logf(ratio);
+    const float back = __builtin_amdgcn_rcpf(ratio);
+    const float lift = kLiftMany + __builtin_amdgcn_logf(ratio);
     f16x8 p[NQ][2], p_low[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {

@@ -72,8 +72,8 @@ struct Code<WM_E4M3> {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI);
   }
   template <bool HI>
-  static __device__ __forceinline__ f16x2 half(uint32_t w, float pow2 = 1.0f) {
-    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, pow2, HI);
+  static __device__ __forceinline__ f16x2 half(uint32_t w) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI);
   }
 };
 template <>
@@ -93,8 +93,8 @@ struct Code<WM_E5M2> {
     return __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, HI);
   }
   template <bool HI>
-  static __device__ __forceinline__ f16x2 half(uint32_t w, float pow2 = 1.0f) {
-    return __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, pow2, HI);
+  static __device__ __forceinline__ f16x2 half(uint32_t w) {
+    return __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(w, 1.0f, HI);
   }
 };
 
@@ -109,10 +109,10 @@ __device__ __forceinline__ uint32_t take_special(u32x4 &x, int j) {
 
 // A request as attention sees it.  Its query rows that share a key head are its
 // tokens times the heads of the group, row = token * group + head; tiles of
-// `rows` of them are worked on together.  Its sequence is cut into parts of 2^cut tokens
-// (512, or more where the span that some row sees has over 30 of them), at
-// multiples of that: the cut depends on the request alone, so a request of
-// one tile gives the same bits whatever else the call holds.
+// `rows` of them are worked on together.  Its sequence is cut into parts of
+// 2^cut tokens (512, or more where the span that some row sees has over 30 of
+// them), at multiples of that: the cut depends on the request alone, so a
+// request of one tile gives the same bits whatever else the call holds.
 struct Request {
   int64_t q0;             // its first query row's token
   uint32_t n_rows, tiles;
@@ -216,13 +216,6 @@ struct Qk<WM_FP16, FMT> {
   static __device__ __forceinline__ frag key(uint32_t x, uint32_t y) {
     const f16x2 p = Code<FMT>::template half<false>(x), q = Code<FMT>::template half<true>(x);
     const f16x2 r = Code<FMT>::template half<false>(y), s = Code<FMT>::template half<true>(y);
-    return frag{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-  }
-  // eight values times a power of two
-  static __device__ __forceinline__ frag value(uint32_t x, uint32_t y, float pow2) {
-    typedef Code<FMT> C;
-    const f16x2 p = C::template half<false>(x, pow2), q = C::template half<true>(x, pow2);
-    const f16x2 r = C::template half<false>(y, pow2), s = C::template half<true>(y, pow2);
     return frag{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
   }
   static __device__ __forceinline__ f32x4 mma(frag k, frag q, f32x4 c) {

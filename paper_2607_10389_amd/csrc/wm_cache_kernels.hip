@@ -242,9 +242,9 @@ __device__ __forceinline__ void load_eight(const void *p, uint64_t at, float *x)
 
 // A block that gets tokens, a head, keys or values: the largest magnitude
 // first, then the codes, from the same 16-byte loads (the second time from
-// L2).  NT threads work on it: a workgroup where blocks get many tokens, a wave where
-// they get a few (a step's single tokens: no barrier, and four times as many
-// blocks on their way).  Keys are stored as they come.  Values are
+// L2).  NT threads work on it: a workgroup where blocks get many tokens, a wave
+// where they get a few (a step's single tokens: no barrier, and four times as
+// many blocks on their way).  Keys are stored as they come.  Values are
 // transposed in registers: a thread takes four tokens of eight dimensions and
 // stores eight words of four tokens, its neighbours the next four tokens, so
 // that 16 threads read 64 bytes of a row and write 64 bytes of one.  What
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   const uint64_t base = (uint64_t)h * bt * dim;
   if ((__float_as_uint(now) & 0x7FFFFFu) != 0) {
     // the caller's own scale, no power of two: true quotients, a byte at a time
-    uint8_t *codes = value ? (uint8_t *)a.c.v + page * a.c.v_stride : (uint8_t *)a.c.k + page * a.c.k_stride;
-    codes += base;
+    uint8_t *codes = (value ? (uint8_t *)a.c.v + page * a.c.v_stride
+                            : (uint8_t *)a.c.k + page * a.c.k_stride) + base;
 #pragma unroll 1
     for (uint32_t i = tid; i < bt * dim; i += NT) {
       const uint32_t t = value ? i & (bt - 1) : i / dim, d = value ? i >> a.bt_log2 : i % dim;
@@ -357,7 +357,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   }
   uint8_t *codes = (uint8_t *)a.c.v + page * a.c.v_stride + base;
   const bool all = fresh || again;
-  const uint32_t g0 = all ? 0u : off / 4, g1 = all ? bt / 4 : (off + n_new + 3) / 4;  // groups of four tokens
+  // groups of four tokens
+  const uint32_t g0 = all ? 0u : off / 4, g1 = all ? bt / 4 : (off + n_new + 3) / 4;
   const uint32_t ng = g1 - g0;
   for (uint32_t i = tid; i < ng * d8; i += NT) {
     const uint32_t t = (g0 + i % ng) * 4, d = i / ng * 8;
@@ -409,7 +410,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
 template <int DT, int KD>
 __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
   const uint32_t hq_all = a.group * a.c.n_heads;
-  const uint64_t at = (uint64_t)blockIdx.x * (kAttThreads / 64) + (threadIdx.x >> 6);
+  const uint64_t unit = (uint64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const uint64_t at = unit * (kAttThreads / 64) + (threadIdx.x >> 6);
   const uint64_t token = at / hq_all;
   if (token >= a.n_tokens) return;
   const uint32_t hq = (uint32_t)(at - token * hq_all);
@@ -576,7 +578,10 @@ int launch_cache_attend(const AttendArgs &a, void *stream) {
   if (e || a.plan.splits <= 1) return e;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint64_t waves = (uint64_t)a.n_tokens * a.group * a.c.n_heads;
-  const uint32_t grid = (uint32_t)((waves + kAttThreads / 64 - 1) / (kAttThreads / 64));
+  const uint32_t units = (uint32_t)((waves + kAttThreads / 64 - 1) / (kAttThreads / 64));
+  // (one axis of a grid holds 2^32 threads)
+  const uint32_t most = 1u << 22;
+  const dim3 grid(units < most ? units : most, (units + most - 1) / most);
   const bool bf = a.q.dtype == WM_BF16;
   switch (d / 64) {
 #define WM_JOIN(kd)                                                      \

@@ -9,6 +9,11 @@ requests room for their new tokens (or takes it back), ``append`` and
 layer's blocks, which a ``Mover`` ships like any other, into whichever blocks
 the destination has free.  The session's answers after a move are the same
 bits as before it: they do not depend on where its blocks lie.
+
+``append`` and ``attend`` may be captured into a graph after they have run
+once at the sizes to come: the slot map and the workspace grow with a step's
+tokens and the longest sequence, and a graph keeps the ones it was captured
+with.  They OR their findings into ``verdict``, which the next ``step`` writes.
 """
 from __future__ import annotations
 
@@ -70,7 +75,8 @@ class PagedCache:
         if bits:
             raise _wm.WmError(_wm.WM_ERR_CAPACITY, f"step (verdict {bits})")
         self.pool, self._pool_next = self._pool_next, self.pool
-        self.lens, self.lengths, self.slot_map = new, want, slots
+        self.lens.copy_(new)  # (captured calls read it where it is)
+        self.lengths, self.slot_map = want, slots
         return tokens
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
@@ -118,6 +124,8 @@ class PagedCache:
         say) is 0 on the device.  The next call is a step()."""
         if self.lengths[request]:
             raise ValueError(f"request {request} holds a session")
+        if flat.numel() * flat.element_size() < self.flat_bytes(length):
+            raise ValueError(f"flat is no state of {length} tokens")
         self.step({request: length})
         n = self._blocks(length)
         if verdict is None:

@@ -781,3 +781,54 @@ def test_calls_on_two_streams_at_once(wm):
             wm.cache_attend(q, *args, o, w, max_len=3000, scale=0.1, stream=s)
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+@pytest.mark.parametrize("n", [100, 600])
+def test_every_request_of_prompts_tells_of_its_length(wm, n):
+    bt, each = 16, 40
+    k, v, ks, vs = make_cache(4, 1, bt, 64, E4, 50)
+    q = torch.randn(n * each, 1, 64).to(BF).cuda()
+    table = dev([[0, 1, 2, 3]] * n)
+    starts = dev([each * i for i in range(n + 1)])
+    for last, want in ((64, 0), (65, 1)):
+        say(f"[attend] the last of {n} requests has {last} tokens")
+        out, verdict = torch.zeros_like(q), word()
+        wm.cache_attend(q, k, v, ks, vs, table, dev([each] * (n - 1) + [last]), starts, out,
+                        max_len=64, scale=0.2, verdict=verdict)
+        assert verdict.item() == want
+
+
+@pytest.mark.parametrize("lens,new,heads,group,bt,dim,dt,fmt,window,low", [
+    ([500, 300], [500, 300], 1, 1, 64, 128, BF, E4, 32, -40),
+    ([400], [400], 2, 2, 64, 64, HF, E5, 40, -60),
+    ([600], [200], 1, 1, 128, 192, BF, E4, 50, -60),
+    ([520], [300], 1, 1, 256, 256, HF, E4, 50, -20),
+    ([300], [300], 1, 1, 16, 64, BF, E4, 10, -12),
+    ([700, 90, 210], [1, 1, 1], 2, 4, 64, 128, HF, E4, 20, -40),
+    ([700, 333], [3, 9], 1, 1, 64, 64, BF, E5, 20, -60),
+    ([300, 129], [20, 9], 1, 1, 128, 256, BF, E4, 20, -60),
+    ([256, 200], [8, 1], 1, 2, 32, 128, HF, E4, 0, -40),
+])
+def test_values_of_very_different_scales(wm, lens, new, heads, group, bt, dim, dt, fmt, window,
+                                         low):
+    """Every other block's values are 2^low times smaller: rows whose window
+    lies in such a block are as precise as the others."""
+    def tail(k, v, ks, vs, rows):
+        for row in rows:
+            for b in row[1::2]:
+                if b >= 0:
+                    vs[b] *= 2.0 ** low
+
+    check_attend(wm, lens, new, heads, group, bt, dim, dt, fmt, window=window, seed=60, tail=tail)
+
+
+def test_a_resume_of_too_small_a_state_changes_nothing():
+    from paper_2607_10389_amd.paged import PagedCache
+    c = PagedCache(1, 8, 1, 64, 16, max_requests=2)
+    c.step({0: 20})
+    flat = c.suspend(0)
+    with pytest.raises(ValueError):
+        c.resume(1, 33, flat)
+    assert c.lengths == [20, 0] and c.pool.tolist()[1] == 6
+    c.resume(1, 20, flat)
+    assert c.lengths == [20, 20] and c.lens.tolist() == [20, 20]
