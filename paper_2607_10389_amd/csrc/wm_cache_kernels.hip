@@ -32,62 +32,101 @@ struct Step {
   }
 };
 
-__device__ __forceinline__ Step step_of(const TablesArgs &a, uint32_t r) {
-  Step s = {0, 0, 0, 0};
-  if (r >= a.n_requests) return s;
-  s.o = a.old_len[r];
-  s.n = a.new_len[r];
+__device__ __forceinline__ Step step_of(const TablesArgs &a, int32_t o, int32_t n) {
   const uint32_t round = (1u << a.bt_log2) - 1u;
-  s.b = (uint32_t)(((uint64_t)(uint32_t)s.o + round) >> a.bt_log2);
-  s.c = (uint32_t)(((uint64_t)(uint32_t)s.n + round) >> a.bt_log2);
-  return s;
+  return Step{o, n, (uint32_t)(((uint64_t)(uint32_t)o + round) >> a.bt_log2),
+              (uint32_t)(((uint64_t)(uint32_t)n + round) >> a.bt_log2)};
+}
+
+// Sums stop at 2^32 - 1: more than any pool or slot map holds.
+__device__ __forceinline__ uint32_t add(uint32_t x, uint32_t y) {
+  return __builtin_elementwise_add_sat(x, y);
+}
+
+// PER lengths from request r on; 0 behind the last request.
+template <int PER>
+__device__ __forceinline__ void load_lengths(const int32_t *p, uint32_t r, uint32_t n, bool wide,
+                                             int32_t *x) {
+  if (PER == 8 && wide && r + PER <= n) {
+    const u32x4 u = *(const u32x4 *)(p + r), v = *(const u32x4 *)(p + r + 4);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) x[i] = (int32_t)(i < 4 ? u[i & 3] : v[i & 3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) x[i] = r + i < n ? p[r + i] : 0;
+}
+
+template <int PER>
+__device__ __forceinline__ void store_entries(uint32_t *to, const uint32_t *x) {
+  if (PER % 4) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) to[i] = x[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER / 4; ++i)
+      ((u32x4 *)to)[i] = u32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+  }
 }
 
 // A thread scans PER neighbouring requests by itself before the waves do.
 constexpr int kTabThreads = 256;
 
+// Neighbouring slots that a workgroup writes: eight a thread, one where there
+// are few (a step's single tokens: latency).
+__host__ __device__ __forceinline__ uint32_t slot_run(uint64_t slot_cap) {
+  return slot_cap <= 8192 ? kTabThreads : 8 * kTabThreads;
+}
+template <int N>
+struct Copies {
+  static constexpr int value = N;
+};
+
 template <int PER>
 __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
   constexpr int NT = kTabThreads, kTile = NT * PER;
-  __shared__ uint64_t sum[3][NT / 64];
-  __shared__ uint32_t pre[3][kTile + 1];
-  __shared__ Step st[kTile];
+  __shared__ uint32_t sum[3][NT / 64];
+  // lengths before and after, and what stands before a request; a thread's PER
+  // entries are written in 16-byte pieces
+  __shared__ __attribute__((aligned(16))) uint32_t st[2][kTile];
+  __shared__ __attribute__((aligned(16))) uint32_t pre[3][kTile + 4];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const uint32_t head = a.pool_in[0], count = a.pool_in[1];
   // tokens, blocks taken and blocks returned in all
-  uint64_t total[3] = {0, 0, 0};
+  uint32_t total[3] = {0, 0, 0};
   auto decide = [&](bool bad) -> bool {
     uint32_t v = 0;
-    if (total[1] > count || count + total[2] > a.ring_cap || head >= a.ring_cap) v |= WM_C_POOL;
+    if (total[1] > count || (uint64_t)count + total[2] > a.ring_cap || head >= a.ring_cap)
+      v |= WM_C_POOL;
     if (total[0] > a.slot_cap) v |= WM_C_SLOTS;
     if (bad) v = WM_C_LENGTH;  // the other counts mean nothing then
     if (blockIdx.x == 0 && tid == 0) {
       *a.verdict = v;
-      a.pool_out[0] = v ? head : (uint32_t)((head + total[1]) % a.ring_cap);
-      a.pool_out[1] = v ? count : (uint32_t)(count - total[1] + total[2]);
+      a.pool_out[0] = v ? head : (uint32_t)(((uint64_t)head + total[1]) % a.ring_cap);
+      a.pool_out[1] = v ? count : count - total[1] + total[2];
       if (!v) a.q_start[a.n_requests] = (int32_t)total[0];
     }
     return v == 0;
   };
   const bool once = a.n_requests <= kTile;
   if (!once) {
-    uint64_t x[3] = {0, 0, 0};
+    uint32_t x[3] = {0, 0, 0};
     bool bad = false;
     for (uint32_t r = tid; r < a.n_requests; r += NT) {
-      const Step s = step_of(a, r);
+      const Step s = step_of(a, a.old_len[r], a.new_len[r]);
       bad |= s.bad(a);
-      x[0] += s.tokens();
-      x[1] += s.need();
-      x[2] += s.give();
+      x[0] = add(x[0], s.tokens());
+      x[1] = add(x[1], s.need());
+      x[2] = add(x[2], s.give());
     }
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      for (int i = 32; i; i >>= 1) x[k] += __shfl_xor(x[k], i);
+      for (int i = 32; i; i >>= 1) x[k] = add(x[k], __shfl_xor(x[k], i));
       if (lane == 0) sum[k][wave] = x[k];
     }
     bad = __syncthreads_or(bad);
     for (int k = 0; k < 3; ++k)
-      for (int i = 0; i < NT / 64; ++i) total[k] += sum[k][i];
+      for (int i = 0; i < NT / 64; ++i) total[k] = add(total[k], sum[k][i]);
     if (!decide(bad)) return;
   }
   const uint64_t step = (uint64_t)gridDim.x * NT;
@@ -95,28 +134,32 @@ __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
   const uint32_t bt = 1u << a.bt_log2;
   // a place of the ring: less than two rounds
   auto place = [&](uint64_t x) { return (uint32_t)(x >= a.ring_cap ? x - a.ring_cap : x); };
-  uint64_t base[3] = {0, 0, 0};
+  const bool wide = (((uintptr_t)a.old_len | (uintptr_t)a.new_len) & 15u) == 0;
+  uint32_t base[3] = {0, 0, 0};
   for (uint32_t r0 = 0; r0 < a.n_requests || (once && r0 == 0); r0 += kTile) {
     __syncthreads();  // the tile before is done with the shared arrays
     Step s[PER];
-    uint64_t x[3] = {0, 0, 0};
+    int32_t o[PER], n[PER];
+    load_lengths<PER>(a.old_len, r0 + PER * tid, a.n_requests, wide, o);
+    load_lengths<PER>(a.new_len, r0 + PER * tid, a.n_requests, wide, n);
+    uint32_t x[3] = {0, 0, 0};
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) s[i] = step_of(a, r0 + PER * tid + i);
-#pragma unroll
     for (int i = 0; i < PER; ++i) {
-      st[PER * tid + i] = s[i];
+      s[i] = step_of(a, o[i], n[i]);
       bad |= s[i].bad(a);
-      x[0] += s[i].tokens();
-      x[1] += s[i].need();
-      x[2] += s[i].give();
+      x[0] = add(x[0], s[i].tokens());
+      x[1] = add(x[1], s[i].need());
+      x[2] = add(x[2], s[i].give());
     }
-    const uint64_t own[3] = {x[0], x[1], x[2]};
+    store_entries<PER>(&st[0][PER * tid], (const uint32_t *)o);
+    store_entries<PER>(&st[1][PER * tid], (const uint32_t *)n);
+    const uint32_t own[3] = {x[0], x[1], x[2]};
     for (int i = 1; i < 64; i <<= 1)
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        const uint64_t y = __shfl_up(x[k], i);
-        if (lane >= i) x[k] += y;
+        const uint32_t y = __shfl_up(x[k], i);
+        x[k] = lane >= i ? add(x[k], y) : x[k];
       }
     if (lane == 63)
 #pragma unroll
@@ -124,19 +167,20 @@ __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
     bad = __syncthreads_or(bad);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-      uint64_t before = base[k], all = base[k];
+      uint32_t before = base[k], all = base[k];
 #pragma unroll
       for (int i = 0; i < NT / 64; ++i) {
-        if (i < wave) before += sum[k][i];
-        all += sum[k][i];
+        if (i < wave) before = add(before, sum[k][i]);
+        all = add(all, sum[k][i]);
       }
-      // (32 bits: enough once decide() has passed)
-      uint32_t p = (uint32_t)(before + x[k] - own[k]);
+      // (exact once decide() has passed)
+      uint32_t p = before + x[k] - own[k], e[PER];
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        pre[k][PER * tid + i] = p;
+        e[i] = p;
         p += k == 0 ? s[i].tokens() : (k == 1 ? s[i].need() : s[i].give());
       }
+      store_entries<PER>(&pre[k][PER * tid], e);
       if (tid == NT - 1) pre[k][kTile] = p;
       if (once) total[k] = all;
       base[k] = all;
@@ -146,6 +190,8 @@ __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
     if (blockIdx.x == 0)
       for (uint32_t i = tid; i < kTile && r0 + i < a.n_requests; i += NT)
         a.q_start[r0 + i] = (int32_t)pre[0][i];
+    // blocks of a length (as in step_of)
+    auto blocks_of = [&](uint32_t n) { return (n + (bt - 1u)) >> a.bt_log2; };
     auto owner = [&](int k, uint32_t j) {  // the last request whose part begins at or before j
       int lo = 0;
 #pragma unroll
@@ -155,23 +201,66 @@ __global__ __launch_bounds__(kTabThreads) void k_page_tables(TablesArgs a) {
     };
     for (uint64_t j = pre[1][0] + at; j < pre[1][kTile]; j += step) {
       const int i = owner(1, (uint32_t)j);
-      a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].b + ((uint32_t)j - pre[1][i])] =
+      a.table[(uint64_t)(r0 + i) * a.table_stride + blocks_of(st[0][i]) +
+              ((uint32_t)j - pre[1][i])] =
           a.ring[place(head + j)];
     }
     for (uint64_t j = pre[2][0] + at; j < pre[2][kTile]; j += step) {
       const int i = owner(2, (uint32_t)j);
       a.ring[place((uint64_t)place((uint64_t)head + count) + j)] =
-          a.table[(uint64_t)(r0 + i) * a.table_stride + st[i].c + ((uint32_t)j - pre[2][i])];
+          a.table[(uint64_t)(r0 + i) * a.table_stride + blocks_of(st[1][i]) +
+                  ((uint32_t)j - pre[2][i])];
     }
-#pragma unroll 4
-    for (uint64_t j = pre[0][0] + at; j < pre[0][kTile]; j += step) {
-      const int i = owner(0, (uint32_t)j);
-      const uint32_t p = (uint32_t)st[i].o + ((uint32_t)j - pre[0][i]);
-      const uint32_t blk = p >> a.bt_log2;
-      const int32_t id = blk < st[i].b
-                             ? a.table[(uint64_t)(r0 + i) * a.table_stride + blk]
-                             : a.ring[place((uint64_t)head + pre[1][i] + (blk - st[i].b))];
-      a.slots[j] = (int64_t)id * bt + (p & (bt - 1u));
+    // the same for the wave: 64 candidates at a time
+    auto owner_of = [&](uint32_t j) {
+      constexpr int kStride = kTile / 64;
+      const int c = __popcll(__ballot(pre[0][lane * kStride] <= j)) - 1;
+      const bool le = lane < kStride && pre[0][c * kStride + lane % kStride] <= j;
+      return c * kStride + __popcll(__ballot(le)) - 1;
+    };
+    // a run of neighbouring slots belongs to few of many requests: a slot's
+    // is searched among those
+    const uint32_t slots1 = pre[0][kTile], n_run = slot_run(a.slot_cap);
+    for (uint64_t run = pre[0][0] + (uint64_t)blockIdx.x * n_run; run < slots1;
+         run += (uint64_t)gridDim.x * n_run) {
+      const uint32_t j0 = (uint32_t)run;
+      const uint32_t j1 = slots1 - j0 < n_run ? slots1 - 1 : j0 + n_run - 1;
+      int lo = 0, hi = kTile - 1, half = kTile / 2;
+      if (PER > 1) {
+        lo = owner_of(j0);
+        hi = owner_of(j1);
+        half = hi > lo ? 1 << (31 - __clz(hi - lo)) : 0;
+      }
+      auto write = [&](auto copies) {  // so many slots a thread, side by side
+        constexpr int N = decltype(copies)::value;
+        uint32_t j[N], p[N];
+        int l[N];
+        int32_t id[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          j[i] = j0 + i * NT + tid < j1 ? j0 + i * NT + tid : j1;
+          l[i] = lo;
+        }
+        for (int m = half; m; m >>= 1)
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (l[i] + m <= hi && pre[0][l[i] + m] <= j[i]) l[i] += m;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const uint32_t o = st[0][l[i]], b = blocks_of(o);
+          p[i] = o + (j[i] - pre[0][l[i]]);
+          const uint32_t blk = p[i] >> a.bt_log2;
+          id[i] = *(blk < b ? a.table + (uint64_t)(r0 + l[i]) * a.table_stride + blk
+                            : a.ring + place((uint64_t)head + pre[1][l[i]] + (blk - b)));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (j0 + i * NT + tid <= j1) a.slots[j[i]] = (int64_t)id[i] * bt + (p[i] & (bt - 1u));
+      };
+      if (j1 - j0 < NT)
+        write(Copies<1>{});
+      else
+        write(Copies<8>{});
     }
   }
 }
@@ -523,12 +612,11 @@ int last_error() { return (int)hipGetLastError(); }
 
 int launch_page_tables(const TablesArgs &a, void *stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  // a workgroup for each 2048 slots (512 where there are few), at most as many
-  // as 256 CUs hold at once (57 KiB of LDS each); one scan for up to 256 or
-  // 2048 requests
-  const uint64_t per = a.slot_cap <= 8192 ? 512 : 2048;
+  // a workgroup for each run of slots, at most as many as 256 CUs hold at once
+  // (40 KiB of LDS each); one scan for up to 256 or 2048 requests
+  const uint64_t per = slot_run(a.slot_cap);
   uint64_t n = (a.slot_cap + per - 1) / per;
-  n = n < 1 ? 1 : (n > 512 ? 512 : n);
+  n = n < 1 ? 1 : (n > 768 ? 768 : n);
   if (a.n_requests <= 256)
     k_page_tables<1><<<(uint32_t)n, kTabThreads, 0, st>>>(a);
   else

@@ -832,3 +832,44 @@ def test_a_resume_of_too_small_a_state_changes_nothing():
     assert c.lengths == [20, 0] and c.pool.tolist()[1] == 6
     c.resume(1, 20, flat)
     assert c.lengths == [20, 20] and c.lens.tolist() == [20, 20]
+
+
+@pytest.mark.parametrize("n", [8, 260])
+def test_tables_of_sums_beyond_32_bits(wm, n):
+    """Tokens and blocks in all that no 32-bit sum holds: refused."""
+    bt, width = 256, (2 ** 31 - 1) // 256
+    say(f"[tables] n={n} of 2^31 - 256 tokens each")
+    table = torch.empty(n, width, dtype=torch.int32, device="cuda")
+    ring, pool, po = dev([5, 6, 7]), dev([1, 2]), dev([-1, -1])
+    slots, starts, v = dev([-9] * 10, torch.int64), dev([-3] * (n + 1)), dev([77])
+    most = dev([width * bt] * n)
+    wm.page_tables(dev([0] * n), most, bt, table, ring, pool, po, slots, starts, v)
+    assert v.item() == 6 and po.tolist() == [1, 2]
+    wm.page_tables(most, dev([0] * n), bt, table, ring, pool, po, slots, starts, v)
+    assert v.item() == 2 and po.tolist() == [1, 2]
+    assert ring.tolist() == [5, 6, 7] and slots.tolist() == [-9] * 10
+    assert starts.tolist() == [-3] * (n + 1)
+
+
+@pytest.mark.parametrize("first", [0, 1, 2])
+@pytest.mark.parametrize("n", [300, 2050])
+def test_tables_of_lengths_at_any_place(wm, n, first):
+    """Lengths that begin at no 16-byte address, and slots in runs."""
+    g = np.random.default_rng(70 + n)
+    bt, old = 32, g.integers(0, 200, n)
+    new = np.where(g.random(n) < 0.5, old, old + g.integers(0, 120, n))
+    new[n // 2] = 9000
+    up = lambda x: -(-x // bt)  # noqa: E731
+    need = int(np.maximum(0, up(new) - up(old)).sum())
+    width, tokens = up(9000) + 1, int(np.maximum(0, new - old).sum())
+    ring = g.permutation(need + 5).tolist()
+    table = g.integers(0, 1 << 20, (n, width)).tolist()
+    want = ref.tables(old.tolist(), new.tolist(), bt, table, ring, 3, need + 2,
+                      [-1] * (tokens + 4), [-7] * (n + 1))
+    pad = lambda x: dev([9] * first + x.tolist())[first:]  # noqa: E731
+    t, rg, po = dev(table), dev(ring), dev([-1, -1])
+    sl, qs, v = dev([-1] * (tokens + 4), torch.int64), dev([-7] * (n + 1)), word()
+    wm.page_tables(pad(old), pad(new), bt, t, rg, dev([3, need + 2]), po, sl, qs, v)
+    assert v.item() == want[5] == 0
+    assert t.tolist() == want[0] and rg.tolist() == want[1] and po.tolist() == want[2]
+    assert sl.tolist() == want[3] and qs.tolist() == want[4]
