@@ -383,14 +383,22 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   const float was = *sp;
   const bool fresh = off == 0 || !(was >= 0x1p-126f && was <= 3.4028234e38f);
   float amax = 0.0f;
-  for (uint32_t i = tid; i < n_new * d8; i += NT) {
-    float x[8];
-    load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(i / d8) * src.row_stride + i % d8 * 8, x);
+  // (several loads under way: one more of the last piece changes nothing)
+  constexpr int U = NT == 64 ? 1 : 4;
+  for (uint32_t i0 = tid; i0 < n_new * d8; i0 += U * NT) {
+    float x[U][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float y = fabsf(x[j]);
-      if (y <= 3.4028234e38f && y > amax) amax = y;
+    for (int u = 0; u < U; ++u) {
+      const uint32_t i = i0 + u * NT < n_new * d8 ? i0 + u * NT : n_new * d8 - 1;
+      load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(i / d8) * src.row_stride + i % d8 * 8, x[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float y = fabsf(x[u][j]);
+        if (y <= 3.4028234e38f && y > amax) amax = y;
+      }
   }
   for (int i = 32; i; i >>= 1) amax = fmaxf(amax, __shfl_xor(amax, i));
   if (NT > 64) {
@@ -428,19 +436,30 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
     // only the new rows, unless all of the block's change
     const bool all = fresh || again;
     const uint32_t t0 = all ? 0u : off, t1 = all ? bt : off + n_new;
-    for (uint32_t i = t0 * d8 + tid; i < t1 * d8; i += NT) {
-      const uint32_t t = i / d8;
-      u32x2 *to = (u32x2 *)(codes + (uint64_t)i * 8);
-      u32x2 w = {0, 0};
-      if (t >= off && t < off + n_new) {
-        float x[8];
-        load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)(t - off) * src.row_stride + i % d8 * 8, x);
-        w = u32x2{codes_of<FMT>(x, inv), codes_of<FMT>(x + 4, inv)};
-      } else if (again) {
-        const u32x2 y = *to;
-        w = u32x2{moved_codes<FMT>(y[0], ratio), moved_codes<FMT>(y[1], ratio)};
+    for (uint32_t i0 = t0 * d8 + tid; i0 < t1 * d8; i0 += U * NT) {
+      float x[U][8];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // (a place that gets no token takes one of those that do, unused)
+        const uint32_t i = i0 + u * NT;
+        uint32_t t = i / d8;
+        t = t < off ? 0u : (t < off + n_new ? t - off : n_new - 1);
+        load_eight<DT, WIDE>(src.ptr, row0 + (uint64_t)t * src.row_stride + i % d8 * 8, x[u]);
       }
-      *to = w;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t i = i0 + u * NT, t = i / d8;
+        if (i >= t1 * d8) break;
+        u32x2 *to = (u32x2 *)(codes + (uint64_t)i * 8);
+        u32x2 w = {0, 0};
+        if (t >= off && t < off + n_new) {
+          w = u32x2{codes_of<FMT>(x[u], inv), codes_of<FMT>(x[u] + 4, inv)};
+        } else if (again) {
+          const u32x2 y = *to;
+          w = u32x2{moved_codes<FMT>(y[0], ratio), moved_codes<FMT>(y[1], ratio)};
+        }
+        *to = w;
+      }
     }
     return;
   }
