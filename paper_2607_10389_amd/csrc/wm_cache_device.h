@@ -142,7 +142,9 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, b
   x.len = (int32_t)len;
   x.pos0 = (int32_t)p0;
   while (((hi - lo) >> x.cut) >= 31u) ++x.cut;
-  auto parts = [&]() { return (uint32_t)(((uint64_t)hi + (1u << x.cut) - 1) >> x.cut) - (lo >> x.cut); };
+  auto parts = [&]() {
+    return (uint32_t)(((uint64_t)hi + (1u << x.cut) - 1) >> x.cut) - (lo >> x.cut);
+  };
   while (parts() > a.plan.splits) ++x.cut;  // longer than the caller's longest
   x.part0 = lo >> x.cut;
   x.parts = parts();
