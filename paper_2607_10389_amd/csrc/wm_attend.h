@@ -540,19 +540,36 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // run in a loop without masks.
 //
 // Measured: 2,048 new tokens over 16,384 for four sessions, 32 query heads of
-// 128, at 915 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500 to 2,048
-// over 1 to 4,096 in 222 us, 650 TFLOP/s.  A step takes 1.15 us a workgroup,
+// 128, at 890 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500 to 2,048
+// over 1 to 4,096 in 227 us, 640 TFLOP/s.  A step takes 1.15 us a workgroup,
 // of which the matrix cores are busy 0.43; a tile's start and end take about
 // 10 us, a third of it for 64 KiB of queries and results.
 constexpr float kSlack = 4.0f, kLiftMany = 11.0f;
 
 constexpr int many_waves(int d) { return d <= 128 ? 4 : 8; }
 
-// (Written out: fmaxf would first turn each operand's signalling NaN quiet.)
+// (Written out: fmaxf would first turn each operand's signalling NaN quiet.
+// The compiler does not see that this reads its operands, so it does not keep
+// the distance that a matrix instruction's result needs: settled() does, and
+// a maximum that lanes exchange ends with an fmaxf.)
 __device__ __forceinline__ float max3(float x, float y, float z) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
   return r;
+}
+
+// Results of matrix instructions that max3() may read: 16 wait states after
+// the last of them, where the 16 x 16 ones need 11 at most.
+template <int NQ>
+__device__ __forceinline__ void settled(f32x4 (&x)[NQ][4]) {
+  static_assert(NQ <= 2, "named below");
+  if (NQ == 1)
+    asm volatile("s_nop 15" : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]));
+  else
+    asm volatile("s_nop 15"
+                 : "+v"(x[0][0]), "+v"(x[0][1]), "+v"(x[0][2]), "+v"(x[0][3]),
+                   "+v"(x[NQ - 1][0]), "+v"(x[NQ - 1][1]), "+v"(x[NQ - 1][2]),
+                   "+v"(x[NQ - 1][3]));
 }
 
 // The item of a workgroup.  Above 512 requests counting would take longer than
@@ -786,6 +803,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    settled<NQ>(sc);
     const float cs = ks * scale;  // not negative: a row's largest score is its largest sum
     const int first = t0 + 16 * g;
     if (kMasked) {
@@ -808,7 +826,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
 #pragma unroll
       for (int i = 3; i < 15; i += 2)
         y = max3(y, sc[n][i >> 2][i & 3], sc[n][(i + 1) >> 2][(i + 1) & 3]);
-      y = max3(y, sc[n][3][3], sc[n][3][3]) * f;
+      y = fmaxf(y, sc[n][3][3]) * f;
       top[n] = group_max(!kMasked && idv < 0 ? kNegInf : y);
       grows |= top[n] > w.m[n] + kSlack;
     }
