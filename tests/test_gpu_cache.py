@@ -783,7 +783,7 @@ def test_calls_on_two_streams_at_once(wm):
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
 
 
-@pytest.mark.parametrize("n", [100, 600])
+@pytest.mark.parametrize("n", [100, 200, 600])
 def test_every_request_of_prompts_tells_of_its_length(wm, n):
     bt, each = 16, 40
     k, v, ks, vs = make_cache(4, 1, bt, 64, E4, 50)
@@ -873,3 +873,14 @@ def test_tables_of_lengths_at_any_place(wm, n, first):
     assert v.item() == want[5] == 0
     assert t.tolist() == want[0] and rg.tolist() == want[1] and po.tolist() == want[2]
     assert sl.tolist() == want[3] and qs.tolist() == want[4]
+
+
+@pytest.mark.parametrize("lens,new,heads,group,dim,more", [
+    # parts and windows of tiles of 128 rows, a request without a token
+    ([2600, 70, 0], [70, 70, 80], 1, 1, 128, dict(window=1100)),
+    ([4000, 900], [80, 75], 2, 1, 256, dict(max_len=1000)),
+    # 33 to 64 rows a request: few of them, and many
+    ([700, 90], [20, 12], 2, 2, 128, {}),
+    ([90, 40, 130, 64] * 10, [12, 9, 10, 11] * 10, 4, 4, 64, {})])
+def test_prompts_of_either_tile(wm, lens, new, heads, group, dim, more):
+    check_attend(wm, lens, new, heads, group, 32, dim, BF, E4, seed=80, **more)
