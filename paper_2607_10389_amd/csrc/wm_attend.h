@@ -263,7 +263,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
   // products, its values while its own scores are computed: each load has a
   // product and a softmax to arrive in, with one step's registers.  (256
   // dimensions have none left for that.)
-  constexpr bool kAhead = D * NQ <= 256 && D < 256;
+  constexpr bool kAhead = D < 256;
   u32x4 kr[4][KC], vr[VT];
   float ks = 0.0f, vs = 0.0f;
   // blocks that are not there are read at block 0 and masked
@@ -926,10 +926,13 @@ int attend_rows(const AttendArgs &a, hipStream_t st) {
   }
   const uint64_t room = (uint64_t)a.n_cu * resident(D, a.plan.rows / 16);
   const uint32_t grid = (uint32_t)(most < room ? most : room);
-  if (a.plan.rows == 16)
-    k_attend<DT, FMT, D, 1><<<grid, kAttThreads, 0, st>>>(a);
-  else
-    k_attend<DT, FMT, D, 2><<<grid, kAttThreads, 0, st>>>(a);
+  if constexpr (D <= 64) {
+    if (a.plan.rows == 32) {
+      k_attend<DT, FMT, D, 2><<<grid, kAttThreads, 0, st>>>(a);
+      return (int)hipGetLastError();
+    }
+  }
+  k_attend<DT, FMT, D, 1><<<grid, kAttThreads, 0, st>>>(a);
   return (int)hipGetLastError();
 }
 
