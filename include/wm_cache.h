@@ -174,6 +174,9 @@ wm_status wm_cache_append(const wm_cache *cache, const wm_rows *k,
  *   block_table : as for wm_page_tables; entries that no row sees are not
  *                 used.  A block outside the pool is not read: its tokens
  *                 count as unseen and WM_C_PAGE is set
+ *   q_start     : n_requests + 1, ascending.  Starts below 0 or beyond n_tokens
+ *                 set WM_C_SLOTS: the rows that are there stand where the
+ *                 formula says, the others are not computed
  *   len         : n_requests; a length beyond the table's max_blocks sets
  *                 WM_C_LENGTH and counts as that many tokens
  *   max_len     : host: the longest length, for the split of the work; the

@@ -91,6 +91,11 @@ __device__ __forceinline__ void load_queries(const AttendArgs &a, const Request 
   }
 }
 
+// The last token before those that a row at `pos` sees, -1 if there is none.
+__device__ __forceinline__ int before_window(const AttendArgs &a, int pos) {
+  return a.window && pos >= (int)a.window ? pos - (int)a.window : -1;
+}
+
 // A wave's rows into the output, or as part `part` into the workspace if the
 // tile has several.
 template <int DT, int FMT, int D, int NQ>
@@ -147,7 +152,7 @@ struct Item {
 
 struct ItemWalk {
   Request *mine;        // LDS: the wave's 64 requests
-  bool tell;            // say so of lengths beyond the table
+  bool tell;            // say so of lengths beyond the table and starts beyond the rows
   uint64_t base = 0;    // items before them
   uint32_t r0 = 0, n = 0, sum = 0, all = 0;  // a lane's items, with those before it, all 64's
 
@@ -246,7 +251,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
   const int32_t *row = a.table + (uint64_t)r * a.table_stride;
   int low[NQ];  // the last token before those that a row sees
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) low[n] = a.window ? pos[n] - (int)a.window : -1;
+  for (int n = 0; n < NQ; ++n) low[n] = before_window(a, pos[n]);
   bool bad_page = false;
   // the table's entry for token j (a multiple of 16), and the block that it is:
   // -1 if no row sees its 16 tokens.  (The entry is looked at a step later,
@@ -622,6 +627,10 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const uint32_t bt = 1u << a.bt_log2;
   __shared__ Request requests[64 * kWaves];
   Item it;
+  // (starts ascend: those beyond the rows show at either end)
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.verdict &&
+      (a.q_start[0] < 0 || (int64_t)a.q_start[a.n_requests] > (int64_t)a.n_tokens))
+    atomicOr(a.verdict, WM_C_SLOTS);
   if (!find_item(a, requests + 64 * wave, blockIdx.x, &it)) return;
   // (every request with new tokens has an item, whose workgroup speaks for it)
   if (threadIdx.x == 0 && a.verdict && (int64_t)a.len[it.r] > (int64_t)a.max_blocks << a.bt_log2)
@@ -635,7 +644,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   int pos[NQ], low[NQ];
   load_queries<DT, FMT, D, NQ>(a, x, row0, h, q, pos);
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) low[n] = a.window ? pos[n] - (int)a.window : -1;
+  for (int n = 0; n < NQ; ++n) low[n] = before_window(a, pos[n]);
   // a negative factor of the scores goes into the queries
   const float scale = fabsf(a.scale_log2);
   if (a.scale_log2 < 0.0f) {

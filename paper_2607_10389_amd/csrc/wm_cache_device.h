@@ -123,6 +123,8 @@ struct Request {
 __device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, bool tell) {
   Request x = {0, 0, 0, 0, 0, a.plan.cut, 0, 1};
   int64_t q0 = a.q_start[r], q1 = a.q_start[r + 1], len = a.len[r];
+  const int64_t end = q1;  // rows that are not there keep their positions
+  if (tell && a.verdict && (q0 < 0 || q1 > (int64_t)a.n_tokens)) atomicOr(a.verdict, WM_C_SLOTS);
   q0 = q0 > 0 ? q0 : 0;
   q1 = q1 < (int64_t)a.n_tokens ? q1 : (int64_t)a.n_tokens;
   if (q0 >= q1) return x;
@@ -132,7 +134,10 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, b
     if (tell && a.verdict) atomicOr(a.verdict, WM_C_LENGTH);
   }
   len = len > 0 ? len : 0;
-  const int64_t p0 = len - (q1 - q0);
+  // (below -2^30 none of up to 2^30 rows sees anything, and differences of
+  // positions stay within 32 bits)
+  int64_t p0 = len - (end - q0);
+  p0 = p0 > -(1ll << 30) ? p0 : -(1ll << 30);
   const uint32_t lo =
       a.window && p0 + 1 > (int64_t)a.window ? (uint32_t)(p0 + 1 - a.window) : 0u;
   const uint32_t hi = (uint32_t)len;

@@ -884,3 +884,51 @@ def test_tables_of_lengths_at_any_place(wm, n, first):
     ([90, 40, 130, 64] * 10, [12, 9, 10, 11] * 10, 4, 4, 64, {})])
 def test_prompts_of_either_tile(wm, lens, new, heads, group, dim, more):
     check_attend(wm, lens, new, heads, group, 32, dim, BF, E4, seed=80, **more)
+
+
+@pytest.mark.parametrize("lens,starts,rows,dim,window", [
+    ([40], [0, 12], 5, 64, 0),                     # few rows: the reading kernel
+    ([40], [0, 12], 5, 64, 9),
+    ([300, 20], [0, 200, 210], 150, 128, 0),       # prompts
+    ([300, 20], [0, 200, 210], 150, 128, 70),
+    ([2000], [0, 12], 4, 64, 0),                   # parts, joined
+    ([40, 30, 50], [0, 3, 3, 9], 3, 64, 0),        # a request that begins behind the rows
+    ([40, 50, 60], [0, 90, 90, 99], 90, 64, 0),
+    ([300, 50, 60], [0, 200, 200, 209], 200, 64, 0),
+    ([40], [-3, 4], 4, 64, 0),                     # rows before the first
+    ([200], [-30, 100], 100, 64, 33),
+    ([5], [0, 2 ** 31 - 1], 3, 64, 2 ** 31 - 1),   # every row before the sequence
+])
+def test_starts_beyond_the_rows(wm, lens, starts, rows, dim, window):
+    """Rows that are there keep the positions that the starts give them."""
+    say(f"[attend] lens={lens} starts={starts} rows={rows} dim={dim} window={window}")
+    bt, hq = 16, 2
+    table, blocks = layout(lens, bt, 90)
+    k, v, ks, vs = make_cache(blocks, 1, bt, dim, E4, 91)
+    q = torch.randn(rows, hq, dim, generator=torch.Generator().manual_seed(92)).to(BF)
+    out, lse, verdict = torch.zeros(rows, hq, dim, dtype=BF, device="cuda"), \
+        torch.zeros(rows, hq, device="cuda"), word()
+    ws = torch.empty(wm.attend_ws_bytes(q, k, dev(lens), max(lens)), dtype=torch.uint8,
+                     device="cuda")
+    wm.cache_attend(q.cuda(), k, v, ks, vs, dev(table), dev(lens), dev(starts), out, ws,
+                    max_len=max(lens), scale=0.2, window=window, lse=lse, verdict=verdict)
+    assert verdict.item() == 4
+    want, z = torch.zeros(rows, hq, dim, dtype=torch.float64), \
+        torch.full((rows, hq), -math.inf, dtype=torch.float64)
+    weight, sp = torch.zeros_like(want), torch.zeros_like(z)
+    kv, vv = values(k, ks, False), values(v, vs, True)
+    for r, n in enumerate(lens):
+        a, b = max(0, starts[r]), min(rows, starts[r + 1])
+        if a >= b:
+            continue
+        last = n - (starts[r + 1] - b)  # one behind the last row's position
+        if last <= 0:
+            continue
+        got = ref.attend(q[a:b], kv, vv, [table[r]], [last], [0, b - a], bt, 0.2, window)
+        for x, y in zip((want, z, weight, sp), got):
+            x[a:b] = y
+    bo, bl = ref.attend_bound(BF, want, z, weight, sp, max(lens), dim)
+    assert bool(((out.cpu().double() - want).abs() <= bo).all())
+    seen = torch.isfinite(z)
+    assert torch.equal(torch.isneginf(lse.cpu()), ~seen)
+    assert bool(((lse.cpu().double() - z).abs()[seen] <= bl[seen]).all())
