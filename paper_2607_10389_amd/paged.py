@@ -10,10 +10,12 @@ layer's blocks, which a ``Mover`` ships like any other, into whichever blocks
 the destination has free.  The session's answers after a move are the same
 bits as before it: they do not depend on where its blocks lie.
 
-``append`` and ``attend`` may be captured into a graph after they have run
-once at the sizes to come: the slot map and the workspace grow with a step's
-tokens and the longest sequence, and a graph keeps the ones it was captured
-with.  They OR their findings into ``verdict``, which the next ``step`` writes.
+``append`` and ``attend`` may be captured into a graph and replayed after any
+later ``step`` of no more tokens: tables, lengths, slot map and row starts keep
+their addresses, and a workspace that has become too small is kept as long as
+the cache, for the graphs and streams that still use it.  (Calls on different
+streams share it: they have to be ordered.)  ``append`` and ``attend`` OR their
+findings into ``verdict``, which the next ``step`` writes.
 """
 from __future__ import annotations
 
@@ -47,9 +49,13 @@ class PagedCache:
         self.lens = torch.zeros(max_requests, **i32)
         self.lengths = [0] * max_requests  # the same on the host
         self.q_start = torch.zeros(max_requests + 1, **i32)
-        self.slot_map = torch.zeros(0, dtype=torch.int64, device=i32["device"])
+        # no step has more new tokens than the blocks have places
+        places = min(blocks, max_requests * self.block_table.shape[1]) * block_tokens
+        self.slot_map = torch.zeros(min(places, 2 ** 31 - 1), dtype=torch.int64,
+                                    device=i32["device"])
         self.verdict = torch.zeros(1, **i32)
         self._ws = torch.zeros(0, dtype=torch.uint8, device=i32["device"])
+        self._outgrown = []  # smaller workspaces
         self.pools = _cache.PoolTable([self.codes, self.scales])
 
     def layer(self, n: int):
@@ -66,17 +72,15 @@ class PagedCache:
             want[r] = n
         tokens = sum(max(0, n - o) for o, n in zip(self.lengths, want))
         new = torch.tensor(want, dtype=torch.int32).to(self.lens.device)
-        slots = self.slot_map
-        if slots.numel() < tokens:
-            slots = torch.zeros(tokens, dtype=torch.int64, device=self.lens.device)
         _cache.page_tables(self.lens, new, self.block_tokens, self.block_table, self.ring,
-                           self.pool, self._pool_next, slots, self.q_start, self.verdict)
+                           self.pool, self._pool_next, self.slot_map[:tokens], self.q_start,
+                           self.verdict)
         bits = int(self.verdict.item())
         if bits:
             raise _wm.WmError(_wm.WM_ERR_CAPACITY, f"step (verdict {bits})")
         self.pool, self._pool_next = self._pool_next, self.pool
         self.lens.copy_(new)  # (captured calls read it where it is)
-        self.lengths, self.slot_map = want, slots
+        self.lengths = want
         return tokens
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
@@ -91,7 +95,10 @@ class PagedCache:
         most = max(self.lengths)
         need = _cache.attend_ws_bytes(q, c[0], self.lens, most)
         if self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            # at least twice as large: the smaller ones together are no larger
+            self._outgrown.append(self._ws)
+            self._ws = torch.empty(max(need, 2 * self._ws.numel()), dtype=torch.uint8,
+                                   device=q.device)
         out = torch.empty_like(q) if out is None else out
         _cache.cache_attend(q, *c, self.block_table, self.lens, self.q_start, out, self._ws,
                             max_len=most, scale=scale, window=window, lse=lse,

@@ -932,3 +932,54 @@ def test_starts_beyond_the_rows(wm, lens, starts, rows, dim, window):
     seen = torch.isfinite(z)
     assert torch.equal(torch.isneginf(lse.cpu()), ~seen)
     assert bool(((lse.cpu().double() - z).abs()[seen] <= bl[seen]).all())
+
+
+def test_a_captured_step_outlives_larger_ones():
+    """A decoding step of a PagedCache, captured, replayed before and after a
+    prompt that needs a larger workspace and more slots: each replay against
+    the eager step of a second cache."""
+    from paper_2607_10389_amd import PagedCache
+    args = dict(layers=1, blocks=420, heads=2, dim=64, block_tokens=16, max_requests=3)
+    c, twin = PagedCache(**args), PagedCache(**args)
+    g = torch.Generator(device="cuda").manual_seed(7)
+
+    def inputs(n):
+        return torch.randn(n, 12, 64, generator=g, device="cuda").to(BF)
+
+    def calls(cache, x, out=None):
+        cache.append(0, x[:, 8:10], x[:, 10:])
+        return cache.attend(0, x[:, :8], 0.125, out=out)
+
+    def both(lengths):
+        n = c.step(lengths)
+        assert twin.step(lengths) == n
+        return n
+
+    x = inputs(both({0: 600, 1: 30}))
+    calls(c, x), calls(twin, x)
+    x = inputs(both({0: 601, 1: 31}))
+    out = torch.zeros(2, 8, 64, dtype=BF, device="cuda")
+    calls(c, x, out), calls(twin, x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(c, x, out)
+    junk = []
+    for i in range(8):
+        if i == 3:
+            y = inputs(both({2: 5000}))
+            a, b = calls(c, y), calls(twin, y)
+            assert torch.equal(a, b)
+            # (a freed buffer would be given out here)
+            junk = [torch.full((1 << k,), 0x55, dtype=torch.uint8, device="cuda")
+                    for k in range(6, 24) for _ in range(4)]
+        both({0: 602 + i, 1: 32 + i})
+        x.copy_(inputs(2))
+        out.zero_()
+        graph.replay()
+        want = calls(twin, x)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and bool(out.any()), i
+        assert torch.equal(c.codes, twin.codes) and torch.equal(c.scales, twin.scales), i
+        assert c.verdict.item() == 0
+        assert all(bool((t == 0x55).all()) for t in junk), i

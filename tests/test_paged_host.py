@@ -1,0 +1,90 @@
+"""PagedCache's host logic without a GPU: its calls of the binding are replaced
+by plain ones on host tensors."""
+import os
+import weakref
+
+import pytest
+import torch
+
+import cache_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2607_10389_amd", "libwm.so")
+
+
+class Calls(list):
+    """(name, address of the slot map or the workspace) of each call."""
+
+
+@pytest.fixture
+def paged(monkeypatch):
+    if not os.path.exists(LIB):
+        pytest.skip("libwm.so is not built")
+    from paper_2607_10389_amd import _cache, paged
+    calls = Calls()
+
+    def page_tables(old, new, bt, table, ring, pool_in, pool_out, slots, starts, verdict,
+                    stream=None):
+        head, count = pool_in.tolist()
+        got = ref.tables(old.tolist(), new.tolist(), bt, table.tolist(), ring.tolist(), head,
+                         count, slots.tolist(), starts.tolist())
+        for t, x in zip((table, ring, pool_out, slots, starts), got):
+            t.copy_(torch.tensor(x, dtype=t.dtype).reshape(t.shape))
+        verdict.fill_(got[5])
+
+    def cache_append(k, v, kc, vc, ks, vs, slots, starts, verdict=None, stream=None):
+        calls.append(("append", slots.data_ptr()))
+
+    def cache_attend(q, kc, vc, ks, vs, table, lens, starts, out, ws=None, **kw):
+        calls.append(("attend", ws.data_ptr()))
+
+    for f in (page_tables, cache_append, cache_attend):
+        monkeypatch.setattr(_cache, f.__name__, f)
+    monkeypatch.setattr(_cache, "PoolTable", lambda pools: pools)
+    paged.calls = calls
+    return paged
+
+
+def small(paged, **kw):
+    args = dict(layers=1, blocks=400, heads=2, dim=64, block_tokens=16, max_requests=3,
+                device="cpu")
+    return paged.PagedCache(**{**args, **kw})
+
+
+def rows(n, heads=2):
+    return torch.zeros(n, heads, 64, dtype=torch.bfloat16)
+
+
+def test_a_larger_step_leaves_the_buffers_of_captured_calls(paged):
+    """What a captured append reads is what every later step writes, and what a
+    captured attend writes belongs to nobody else."""
+    c = small(paged)
+    c.step({0: 600})
+    c.step({0: 601})
+    c.append(0, rows(1), rows(1))
+    c.attend(0, rows(1, 8), 0.1)
+    (_, slots), (_, ws) = paged.calls
+    kept = weakref.ref(c._ws)
+    n = c.step({1: 5000})  # more tokens, a longer sequence
+    c.append(0, rows(n), rows(n))
+    c.attend(0, rows(n, 8), 0.1)
+    c.step({0: 602, 1: 5001})
+    c.attend(0, rows(2, 8), 0.1)
+    assert paged.calls[-1][1] != ws
+    assert c.slot_map.data_ptr() == slots == paged.calls[2][1]
+    want = [int(c.block_table[r, p // 16]) * 16 + p % 16 for r, p in ((0, 601), (1, 5000))]
+    assert c.slot_map[:2].tolist() == want
+    assert kept() is not None and kept().data_ptr() == ws
+
+
+def test_the_slot_map_holds_the_largest_step(paged):
+    c = small(paged, blocks=9, max_requests=4)
+    assert c.step({0: 64, 1: 33, 2: 16, 3: 16}) == 129  # all nine blocks
+    c.step({r: 0 for r in range(4)})
+    assert c.step({1: 144}) == 144
+    c = small(paged, blocks=100, max_requests=2, max_blocks=3)
+    assert c.step({0: 48, 1: 48}) == 96
+    from paper_2607_10389_amd import WmError
+    with pytest.raises(WmError):
+        c.step({0: 49})
+    assert c.lengths == [48, 48]
