@@ -14,8 +14,8 @@ bits as before it: they do not depend on where its blocks lie.
 later ``step`` of no more tokens: tables, lengths, slot map and row starts keep
 their addresses, and a workspace that has become too small is kept as long as
 the cache, for the graphs and streams that still use it.  (Calls on different
-streams share it: they have to be ordered.)  ``append`` and ``attend`` OR their
-findings into ``verdict``, which the next ``step`` writes.
+streams share it: they have to be ordered.)  What the calls find on the device
+is ORed into ``verdict`` and stays there until the next ``step`` raises for it.
 """
 from __future__ import annotations
 
@@ -54,6 +54,8 @@ class PagedCache:
         self.slot_map = torch.zeros(min(places, 2 ** 31 - 1), dtype=torch.int64,
                                     device=i32["device"])
         self.verdict = torch.zeros(1, **i32)
+        self._word = torch.zeros(1, **i32)  # a call's own verdict
+        self._tokens = 0  # of the last step
         self._ws = torch.zeros(0, dtype=torch.uint8, device=i32["device"])
         self._outgrown = []  # smaller workspaces
         self.pools = _cache.PoolTable([self.codes, self.scales])
@@ -66,31 +68,46 @@ class PagedCache:
         """Take requests to new lengths (0: done); the others stay.  Returns
         the number of new tokens, whose keys, values and queries append() and
         attend() expect ordered by request.  Waits for the verdict; raises
-        WmError, and changes nothing, if the pool or the tables are too small."""
+        WmError, and changes nothing, if the pool or the tables are too small,
+        or (once) if a call since the last step has left a finding."""
         want = list(self.lengths)
         for r, n in new_lengths.items():
             want[r] = n
+        found = int(self.verdict.item())
+        if found:
+            self.verdict.zero_()
+            raise _wm.WmError(_wm.WM_ERR_INVALID_ARG, f"a call before step (verdict {found})")
         tokens = sum(max(0, n - o) for o, n in zip(self.lengths, want))
         new = torch.tensor(want, dtype=torch.int32).to(self.lens.device)
         _cache.page_tables(self.lens, new, self.block_tokens, self.block_table, self.ring,
                            self.pool, self._pool_next, self.slot_map[:tokens], self.q_start,
-                           self.verdict)
-        bits = int(self.verdict.item())
+                           self._word)
+        bits = int(self._word.item())
+        if bits & _cache.C_POOL:
+            bits &= ~_cache.C_SLOTS  # (the slot map is as large as the pool)
         if bits:
             raise _wm.WmError(_wm.WM_ERR_CAPACITY, f"step (verdict {bits})")
         self.pool, self._pool_next = self._pool_next, self.pool
         self.lens.copy_(new)  # (captured calls read it where it is)
-        self.lengths = want
+        self.lengths, self._tokens = want, tokens
         return tokens
 
+    def _rows(self, t: torch.Tensor) -> None:
+        if t.shape[0] < self._tokens:
+            raise ValueError(f"{t.shape[0]} rows for the step's {self._tokens} tokens")
+
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor) -> None:
-        """Store the step's new keys and values [tokens, heads, dim]."""
+        """Store the step's new keys and values [tokens, heads, dim] (rows
+        behind the last token are padding)."""
+        self._rows(k)
         _cache.cache_append(k, v, *self._layers[layer], self.slot_map, self.q_start,
                             self.verdict)
 
     def attend(self, layer: int, q: torch.Tensor, scale: float, window: int = 0,
                out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
-        """Attention of the step's new tokens [tokens, query heads, dim]."""
+        """Attention of the step's new tokens [tokens, query heads, dim] (rows
+        behind the last token are padding, and stay as they are in out)."""
+        self._rows(q)
         c = self._layers[layer]
         most = max(self.lengths)
         need = _cache.attend_ws_bytes(q, c[0], self.lens, most)
@@ -120,8 +137,9 @@ class PagedCache:
         if flat is None:
             flat = torch.empty(self.flat_bytes(self.lengths[request]), dtype=torch.uint8,
                                device=self.codes.device)
-        self.verdict.zero_()
-        _cache.flatten_pages(self.pools, self.block_table[request, :n], flat, self.verdict)
+        self._word.zero_()
+        _cache.flatten_pages(self.pools, self.block_table[request, :n], flat, self._word)
+        self.verdict |= self._word
         return flat
 
     def resume(self, request: int, length: int, flat: torch.Tensor,
@@ -135,7 +153,7 @@ class PagedCache:
             raise ValueError(f"flat is no state of {length} tokens")
         self.step({request: length})
         n = self._blocks(length)
+        word = self._word.zero_() if verdict is None else verdict
+        _cache.rehydrate_pages(flat, self.pools, self.block_table[request, :n], word)
         if verdict is None:
-            self.verdict.zero_()
-            verdict = self.verdict
-        _cache.rehydrate_pages(flat, self.pools, self.block_table[request, :n], verdict)
+            self.verdict |= word

@@ -983,3 +983,30 @@ def test_a_captured_step_outlives_larger_ones():
         assert torch.equal(c.codes, twin.codes) and torch.equal(c.scales, twin.scales), i
         assert c.verdict.item() == 0
         assert all(bool((t == 0x55).all()) for t in junk), i
+
+
+def test_findings_of_a_cache_reach_its_next_step():
+    """A captured append of fewer rows than a later step has tokens: the step
+    after it raises, and the one after that goes on."""
+    from paper_2607_10389_amd import PagedCache, WmError
+    c = PagedCache(layers=1, blocks=20, heads=1, dim=64, block_tokens=16, max_requests=3)
+    x = torch.randn(4, 1, 64, device="cuda").to(BF)
+    c.step({0: 1})
+    c.append(0, x[:1], x[:1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.append(0, x[:1], x[:1])
+    c.step({0: 2, 1: 3})
+    with pytest.raises(ValueError):
+        c.append(0, x[:3], x[:3])
+    graph.replay()
+    flat = c.suspend(0)
+    assert c.verdict.item() == 4
+    before = [t.clone() for t in (c.block_table, c.ring, c.pool, c.lens, c.q_start)]
+    with pytest.raises(WmError):
+        c.step({0: 3})
+    after = (c.block_table, c.ring, c.pool, c.lens, c.q_start)
+    assert all(torch.equal(a, b) for a, b in zip(before, after)) and c.lengths == [2, 3, 0]
+    assert c.step({0: 3}) == 1
+    c.resume(2, 2, flat)
+    assert c.verdict.item() == 0 and torch.equal(c.suspend(2), flat)

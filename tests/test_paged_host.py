@@ -38,10 +38,20 @@ def paged(monkeypatch):
     def cache_attend(q, kc, vc, ks, vs, table, lens, starts, out, ws=None, **kw):
         calls.append(("attend", ws.data_ptr()))
 
-    for f in (page_tables, cache_append, cache_attend):
+    def flatten_pages(pools, pages, flat, verdict, stream=None):
+        calls.append(("flatten", int(verdict.item())))
+        verdict |= paged.found
+
+    def rehydrate_pages(flat, pools, pages, verdict, stream=None):
+        calls.append(("rehydrate", int(verdict.item())))
+        verdict |= paged.found
+
+    for f in (page_tables, cache_append, cache_attend, flatten_pages, rehydrate_pages):
         monkeypatch.setattr(_cache, f.__name__, f)
     monkeypatch.setattr(_cache, "PoolTable", lambda pools: pools)
-    paged.calls = calls
+    monkeypatch.setattr(_cache, "flat_pages_bytes", lambda pools, n: 1024 * n)
+    monkeypatch.setattr(paged, "calls", calls, raising=False)
+    monkeypatch.setattr(paged, "found", 0, raising=False)  # by the page calls
     return paged
 
 
@@ -88,3 +98,44 @@ def test_the_slot_map_holds_the_largest_step(paged):
     with pytest.raises(WmError):
         c.step({0: 49})
     assert c.lengths == [48, 48]
+
+
+def test_findings_stay_until_a_step_raises_for_them(paged):
+    from paper_2607_10389_amd import WmError
+    c = small(paged)
+    c.step({0: 20})
+    c.verdict.fill_(4)  # an append's, say
+    flat = c.suspend(0)
+    assert paged.calls[-1] == ("flatten", 0) and c.verdict.item() == 4
+    state = c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist(), c.slot_map.tolist()
+    with pytest.raises(WmError, match="verdict 4"):
+        c.step({0: 21})
+    assert state == (c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist(),
+                     c.slot_map.tolist())
+    assert c.step({0: 21}) == 1
+    with pytest.raises(WmError, match="verdict 2"):
+        c.step({0: 1 << 12, 1: 1 << 12})
+    assert c.step({0: 22}) == 1  # a refused step leaves no finding
+    paged.found = 8
+    c.suspend(0)
+    assert c.verdict.item() == 8
+    with pytest.raises(WmError, match="verdict 8"):
+        c.step({0: 23})
+    c.resume(1, 20, flat)
+    assert paged.calls[-1] == ("rehydrate", 0) and c.verdict.item() == 8
+
+
+def test_fewer_rows_than_the_step_has_tokens_are_refused(paged):
+    c = small(paged)
+    n = c.step({0: 5, 2: 1})
+    for short in (0, n - 1):
+        with pytest.raises(ValueError):
+            c.append(0, rows(short), rows(short))
+        with pytest.raises(ValueError):
+            c.attend(0, rows(short, 8), 0.1)
+    assert not paged.calls
+    c.append(0, rows(n + 2), rows(n + 2))  # padding
+    c.attend(0, rows(n, 8), 0.1)
+    c.step({0: 6})
+    c.append(0, rows(1), rows(1))
+    assert [x for x, _ in paged.calls] == ["append", "attend", "append"]
