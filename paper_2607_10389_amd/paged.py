@@ -146,11 +146,19 @@ class PagedCache:
                verdict: torch.Tensor | None = None) -> None:
         """Give an empty request blocks for a session of this length and
         install its flat state there, if the verdict word (wm_decode_verify's,
-        say) is 0 on the device.  The next call is a step()."""
+        say) is 0 on the device.  If it is not, the request has its blocks all
+        the same, with nothing installed: step({request: 0}) frees them.  The
+        next call is a step()."""
         if self.lengths[request]:
             raise ValueError(f"request {request} holds a session")
         if flat.numel() * flat.element_size() < self.flat_bytes(length):
             raise ValueError(f"flat is no state of {length} tokens")
+        # (the copy's own checks come behind the step: too late to change nothing)
+        dev = self.lens.get_device()
+        if flat.get_device() != dev or not flat.is_contiguous() or flat.data_ptr() % 16:
+            raise ValueError(f"flat is dense, 16-byte aligned and on device {dev}")
+        if verdict is not None:
+            _cache._word(verdict, dev)
         self.step({request: length})
         n = self._blocks(length)
         word = self._word.zero_() if verdict is None else verdict

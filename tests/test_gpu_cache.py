@@ -1010,3 +1010,21 @@ def test_findings_of_a_cache_reach_its_next_step():
     assert c.step({0: 3}) == 1
     c.resume(2, 2, flat)
     assert c.verdict.item() == 0 and torch.equal(c.suspend(2), flat)
+
+
+def test_a_resume_from_the_host_takes_no_blocks():
+    from paper_2607_10389_amd import PagedCache
+    c = PagedCache(layers=1, blocks=8, heads=1, dim=64, block_tokens=16, max_requests=2)
+    c.step({0: 20})
+    flat = c.suspend(0)
+    state = c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist()
+    for f, v in ((flat.cpu(), None), (flat, torch.zeros(1, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            c.resume(1, 20, f, v)
+        assert state == (c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist())
+    # a verdict that is not zero: blocks, nothing in them, and they go back
+    before = c.codes.clone()
+    c.resume(1, 20, flat, dev([1]))
+    assert c.lengths == [20, 20] and torch.equal(c.codes, before)
+    c.step({1: 0})
+    assert c.pool.tolist()[1] == 6

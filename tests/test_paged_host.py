@@ -139,3 +139,22 @@ def test_fewer_rows_than_the_step_has_tokens_are_refused(paged):
     c.step({0: 6})
     c.append(0, rows(1), rows(1))
     assert [x for x, _ in paged.calls] == ["append", "attend", "append"]
+
+
+def test_a_resume_that_is_refused_takes_no_blocks(paged):
+    c = small(paged)
+    c.step({0: 20})
+    buf = torch.zeros(1 << 14, dtype=torch.uint8)
+    good = buf[-buf.data_ptr() % 16:][:4096]
+    word = torch.zeros(1, dtype=torch.int32)
+    state = c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist(), c.ring.tolist()
+    for flat, verdict in ((good[1:], None), (good[8:], word), (good.view(2, 2048)[:, ::2], word),
+                          (good.view(64, 64).t(), None), (good, word.long()),
+                          (good, torch.zeros(0, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            c.resume(1, 20, flat, verdict)
+    assert not paged.calls
+    assert state == (c.lengths, c.lens.tolist(), c.pool.tolist(), c.q_start.tolist(),
+                     c.ring.tolist())
+    c.resume(1, 20, good, word)
+    assert paged.calls == [("rehydrate", 0)] and c.lengths == [20, 20, 0]
