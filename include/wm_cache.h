@@ -159,7 +159,8 @@ wm_status wm_cache_append(const wm_cache *cache, const wm_rows *k,
  *   lse = log sum_j exp s_j
  * A row that sees nothing (p < 0, a length of 0) gets zeros and lse = -inf.
  * What a row does not see has no influence on it, infinities and NaN
- * included.  Scores, softmax and sums are in 32 bits.  One query row per
+ * included; a value that is not finite reaches every row that sees it, however
+ * small its weight.  Scores, softmax and sums are in 32 bits.  One query row per
  * request is the form for single tokens; many are a prompt or a chunk of it.
  * With up to 32 query heads to a key head, a single token gets the same bits
  * in any call of single tokens whose max_len is not below its length.

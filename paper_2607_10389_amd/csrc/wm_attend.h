@@ -21,6 +21,7 @@ struct Rows {
   float m[NQ], l[NQ];  // maximum of the scores (base 2) and sum of the weights
   float vref;          // o is in units of vref 2^-kLift
   float vtop;          // the largest scale of the values so far
+  bool special;        // (the whole wave's) values that are not finite were added
 };
 
 template <int D, int NQ>
@@ -34,6 +35,7 @@ __device__ __forceinline__ void clear(Rows<D, NQ> *w) {
   }
   w->vref = 0x1p-125f;  // below it a scale has no exact reciprocal
   w->vtop = 0x1p-125f / kUnitLow;
+  w->special = false;
 }
 
 // The unit of the value sums in a step whose largest scale is `most`: the
@@ -194,8 +196,8 @@ struct ItemWalk {
 };
 
 // The values of steps [first, last] that are not finite, for the rows that see
-// them (adding one twice changes nothing).  A cache of finite values never
-// gets here.
+// them (a NaN may be added twice, which changes nothing).  A cache of finite
+// values never gets here.
 template <int FMT, int D, int NQ>
 __device__ __forceinline__ void add_special(const AttendArgs &a, const Tile &t, uint32_t h,
                                             const int32_t *row, uint32_t first, uint32_t last,
@@ -398,19 +400,13 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
       }
       return o;
     };
-    // values that are not finite and that some row does not see: a weight of
-    // 0 would not keep them out of the product.  They are taken out here, and
-    // the rows that see them get them at the end.
-    if (masked) {
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < VT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) any |= take_special<FMT>(vr[i], j);
-      if (__any(any != 0)) {
-        sp_first = s < sp_first ? s : sp_first;
-        sp_last = s;
-      }
+    // values that are not finite: a weight of 0 would not keep those that a
+    // row does not see out of the product, and an infinity would meet weights
+    // that are rounded to 0 or (the second term) below it.  They are taken out
+    // here, and the rows that see them get them at the end.
+    if ((masked || Code<FMT>::kInfinities) && take_special<FMT>(vr)) {
+      sp_first = s < sp_first ? s : sp_first;
+      sp_last = s;
     }
 #pragma unroll
     for (int i = 0; i < VT; ++i)
@@ -422,8 +418,8 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
       entries(s + 8);
     }
   }
-  if (sp_first <= sp_last)
-    add_special<FMT, D, NQ>(a, t, h, row, sp_first, sp_last, pos, low, w);
+  w->special = sp_first <= sp_last;
+  if (w->special) add_special<FMT, D, NQ>(a, t, h, row, sp_first, sp_last, pos, low, w);
   // a lane has summed its own tokens: the rows' sums over the lane groups
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
@@ -438,6 +434,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
 template <int D, int NQ>
 struct Parked {
   float o[NQ * (D / 4)][64], m[NQ][64], l[NQ][64], vref[64];
+  uint32_t special;
 };
 
 template <int D, int NQ>
@@ -452,11 +449,13 @@ __device__ __forceinline__ void park(const Rows<D, NQ> &w, Parked<D, NQ> *x, int
     x->l[n][lane] = w.l[n];
   }
   x->vref[lane] = w.vref;
+  if (lane == 0) x->special = w.special;
 }
 
 template <int D, int NQ>
 __device__ __forceinline__ void join(Rows<D, NQ> *w, const Parked<D, NQ> &x, int lane) {
   const float vx = x.vref[lane], vref = fmaxf(w->vref, vx);
+  w->special |= __builtin_amdgcn_readfirstlane(x.special) != 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const float mx = x.m[n][lane], top = fmaxf(w->m[n], mx);
@@ -465,6 +464,15 @@ __device__ __forceinline__ void join(Rows<D, NQ> *w, const Parked<D, NQ> &x, int
     w->m[n] = top;
     w->l[n] = w->l[n] * f0 + x.l[n][lane] * f1;
     const float g0 = f0 * (w->vref / vref), g1 = f1 * (vx / vref);
+    if (w->special) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w->o[n][i][j] = weighed(g0, w->o[n][i][j]) +
+                          weighed(g1, x.o[n * (D / 4) + 4 * i + j][lane]);
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -621,7 +629,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   constexpr int KS = kWaves / 4, KW = (KC + KS - 1) / KS, VW = (VT + kWaves - 1) / kWaves;
   __shared__ u32x4 kf[2][8 * KC][64];  // [step][4 tiles x 2 KC][lane]
   __shared__ u32x4 vf[2][2 * VT][64];
-  __shared__ uint32_t special[2][kWaves];
+  __shared__ uint32_t special[2][kWaves];  // the waves' sp_first and sp_last
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   const int c16 = lane & 15, g = lane >> 4, ka = c16 >> 2, kb = c16 & 3;
   const uint32_t bt = 1u << a.bt_log2;
@@ -688,7 +696,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   // does the wave have share j of the keys, of the values?
   auto has_k = [&](int j) { return KC % KS == 0 || (wave >> 2) + KS * j < KC; };
   auto has_v = [&](int j) { return VT % kWaves == 0 || wave + kWaves * j < VT; };
-  u32x4 kg[KW], vg[VW];
+  u32x4 kg[KW], vg[VW] = {};
   float ks1 = 0.0f, vs1 = 0.0f;
   int32_t idk1 = -1, idv1 = -1;  // blocks of the step that is loaded
   int32_t ek = 0, ev = 0;        // entries of the one after
@@ -737,7 +745,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     load(s0);
     blocks(s0 + 1);
   }
-  uint32_t sp_first = ~0u, sp_last = 0;  // steps with values that were taken out
+  uint32_t sp_first = ~0u, sp_last = 0;  // steps with values that the wave took out
   auto step = [&](uint32_t s, auto mask_tag) {
     constexpr bool kMasked = decltype(mask_tag)::value;
     const int b = s & 1;
@@ -745,7 +753,6 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     // a block that is not there: no codes that could be NaN, scales of 0
     const float ks = idv < 0 ? 0.0f : ks1, vs = idv < 0 ? 0.0f : vs1;
     const uint32_t k_there = idk1 < 0 ? 0u : ~0u, v_there = idv < 0 ? 0u : ~0u;
-    uint32_t sp = 0;
 #pragma unroll
     for (int j = 0; j < KW; ++j)
       if (has_k(j)) {
@@ -754,21 +761,20 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
         kf[b][at][lane] = __builtin_bit_cast(u32x4, T::key(kg[j][0], kg[j][1]));
         kf[b][at + 1][lane] = __builtin_bit_cast(u32x4, T::key(kg[j][2], kg[j][3]));
       }
+    // (a place without a share is 0 from the start)
+#pragma unroll
+    for (int j = 0; j < VW; ++j) vg[j] &= v_there;
+    if ((kMasked || Code<FMT>::kInfinities) && take_special<FMT>(vg)) {  // as in attend_steps()
+      sp_first = s < sp_first ? s : sp_first;
+      sp_last = s;
+    }
 #pragma unroll
     for (int j = 0; j < VW; ++j)
       if (has_v(j)) {
-        vg[j] &= v_there;
-        if (kMasked)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sp |= take_special<FMT>(vg[j], k);
         const int at = 2 * (wave + kWaves * j);
         vf[b][at][lane] = __builtin_bit_cast(u32x4, V::key(vg[j][0], vg[j][1]));
         vf[b][at + 1][lane] = __builtin_bit_cast(u32x4, V::key(vg[j][2], vg[j][3]));
       }
-    if (kMasked) {
-      sp = __any(sp != 0);
-      if (lane == 0) special[b][wave] = sp;
-    }
     if (s + 1 < s1) {
       load(s + 1);
       blocks(s + 2);
@@ -777,15 +783,6 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     const float ratio = fmaxf(vs * __builtin_amdgcn_rcpf(vref), 0x1p-60f);
     __syncthreads();
     const int t0 = (int)(s << 6);
-    if (kMasked) {
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) any |= special[b][i];
-      if (__builtin_amdgcn_readfirstlane(any)) {
-        sp_first = s < sp_first ? s : sp_first;
-        sp_last = s;
-      }
-    }
     if (kMasked && (t0 >= w_hi || t0 + 63 < w_lo)) return;  // nothing for this wave
     f32x4 sc[NQ][4];
 #pragma unroll
@@ -912,6 +909,19 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       for (; s < end; ++s) step(s, Yes{});
     else
       for (; s < end; ++s) step(s, No{});
+  }
+  // each wave took out of its share, for the rows of all
+  if (lane == 0) {
+    special[0][wave] = sp_first;
+    special[1][wave] = sp_last;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const uint32_t x = __builtin_amdgcn_readfirstlane(special[0][i]);
+    const uint32_t y = __builtin_amdgcn_readfirstlane(special[1][i]);
+    sp_first = x < sp_first ? x : sp_first;
+    sp_last = y > sp_last ? y : sp_last;
   }
   if (sp_first <= sp_last)
     add_special<FMT, D, NQ>(a, t, h, row, sp_first, sp_last, pos, low, &w);

@@ -567,10 +567,10 @@ __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      // a weight of 0 behind the last part
+      // (behind the last part it comes again, with a weight of 0)
       const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), k0 + k));
 #pragma unroll
-      for (int j = 0; j < KD; ++j) o[j] += f == 0.0f ? 0.0f : f * y[k][j];
+      for (int j = 0; j < KD; ++j) o[j] += weighed(f, y[k][j]);
     }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;

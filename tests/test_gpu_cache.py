@@ -1028,3 +1028,38 @@ def test_a_resume_from_the_host_takes_no_blocks():
     assert c.lengths == [20, 20] and torch.equal(c.codes, before)
     c.step({1: 0})
     assert c.pool.tolist()[1] == 6
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("lens,new,heads,group,bt,dim,window", [
+    ([300, 520], [1, 1], 1, 16, 16, 64, 0),      # the reading kernel, rows that see all
+    ([300], [1], 2, 4, 64, 128, 0),
+    ([1200], [1], 1, 16, 32, 64, 0),             # in parts
+    ([700], [1], 1, 16, 16, 256, 400),
+    ([400], [80], 1, 2, 16, 64, 0),              # prompts
+    ([400], [80], 1, 2, 64, 128, 0),
+    ([500], [90], 1, 2, 32, 192, 320),
+    ([400], [80], 1, 2, 128, 256, 0),
+])
+def test_infinite_values_that_every_row_sees(wm, dt, lens, new, heads, group, bt, dim, window):
+    """An infinity stays one whatever its weight, if no other sign meets it."""
+    say(f"[attend] {dt} lens={lens} new={new} {heads}x{group} bt={bt} dim={dim} window={window}")
+    rows, blocks = layout(lens, bt, 95)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, E5, 96)
+    for r, n in enumerate(lens):
+        for off, d, code in ((70, 3, 0x7C), (130, 4, 0xFC), (75, 5, 0x7C), (140, 5, 0xFC)):
+            j = n - new[r] - off  # every row sees it
+            v.view(torch.uint8)[rows[r][j // bt], :, d, j % bt] = code
+    starts = [0] + np.cumsum(new).tolist()
+    q = (torch.randn(starts[-1], heads * group, dim,
+                     generator=torch.Generator().manual_seed(97)) * 8).to(dt).cuda()
+    out = torch.zeros_like(q)
+    ws = torch.empty(wm.attend_ws_bytes(q, k, dev(lens), max(lens)), dtype=torch.uint8,
+                     device="cuda")
+    wm.cache_attend(q, k, v, ks, vs, dev(rows), dev(lens), dev(starts), out, ws,
+                    max_len=max(lens), scale=0.5, window=window)
+    o = out.float().cpu()
+    assert bool((o[..., 3] == math.inf).all())
+    assert bool((o[..., 4] == -math.inf).all())
+    assert bool(o[..., 5].isnan().all())
+    assert bool(torch.isfinite(o[..., [0, 1, 2]]).all()) and bool(torch.isfinite(o[..., 6:]).all())
