@@ -164,10 +164,9 @@ wm_status wm_cache_append(const wm_cache *cache, const wm_rows *k,
  * request is the form for single tokens; many are a prompt or a chunk of it.
  * With up to 32 query heads to a key head, a single token gets the same bits
  * in any call of single tokens whose max_len is not below its length.
- * Weights are rounded to 11 bits for bf16 outputs and 22 for fp16 ones before
- * they meet the values; blocks within 64 tokens may differ 2^12 fold in the
- * scales of their values, others 2^64 fold, and rows that see only the smaller
- * ones lose nothing to that.
+ * Weights, times the scales of their values, are rounded to 11 bits for bf16
+ * outputs and 22 for fp16 ones before they meet the codes; those far below the
+ * row's largest to 2^-35 of it.
  *   q, out      : n_tokens rows of n_q_heads heads, the same type, fewer
  *                 than 2^30 vectors; rows behind the last request's are
  *                 neither read nor written

@@ -6,11 +6,11 @@
 namespace wm {
 namespace {
 
-// exponent that weights are raised by before they are rounded to half
-// precision: at most 2^15 then, and a weight of 2^-29 of the largest still has
-// all its bits (2^-40 its last one)
+// exponent that weights (times their values' scales, in the row's unit) are
+// raised by before they are rounded to half precision: at most 2^15 then, and
+// one of 2^-29 of the largest still has all its bits (2^-40 its last one)
 constexpr float kLift = 15.0f;
-constexpr float kUnitLow = 0x1p-64f;  // see unit_of()
+constexpr float kUnitLeast = -125.0f;  // 2^125 and 2^-125 are both normal numbers
 
 // What a wave holds of its 16 NQ rows.  A lane has one row of each 16 (column
 // lane % 16 of the matrix core's result) and of the output the dimensions
@@ -19,8 +19,7 @@ template <int D, int NQ>
 struct Rows {
   f32x4 o[NQ][D / 16];
   float m[NQ], l[NQ];  // maximum of the scores (base 2) and sum of the weights
-  float vref;          // o is in units of vref 2^-kLift
-  float vtop;          // the largest scale of the values so far
+  float most[NQ];      // maximum of weight times scale (base 2)
   bool special;        // (the whole wave's) values that are not finite were added
 };
 
@@ -30,23 +29,22 @@ __device__ __forceinline__ void clear(Rows<D, NQ> *w) {
   for (int n = 0; n < NQ; ++n) {
     w->m[n] = kNegInf;
     w->l[n] = 0.0f;
+    w->most[n] = kNegInf;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) w->o[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  w->vref = 0x1p-125f;  // below it a scale has no exact reciprocal
-  w->vtop = 0x1p-125f / kUnitLow;
   w->special = false;
 }
 
-// The unit of the value sums in a step whose largest scale is `most`: the
-// largest scale so far, as a rule.  Weights are rounded to half precision in
-// that unit, so where a step's scales are over 2^6 below it, the unit comes
-// down to them, by 2^64 from the largest at most: the sums, up to 2^57 units
-// over 2^26 tokens, cannot overflow.
-__device__ __forceinline__ float unit_of(float unit, float most, float *top) {
-  *top = fmaxf(*top, most);
-  const bool low = most > 0.0f && most < unit * 0x1p-6f;
-  return fmaxf(low ? *top * kUnitLow : unit, most);
+__device__ __forceinline__ float or_zero(float x) { return x == kNegInf ? 0.0f : x; }
+
+// The unit of a row's value sums, 2^(unit - kLift) with a whole number, where
+// `most` is the largest weight times scale of what the row has seen (base 2, as
+// scores are) and `top` its largest score.  So the parts that make up the sum
+// are rounded to half precision with all their bits, whether the weight is
+// large or the scale, and what the row does not see has no say in it.
+__device__ __forceinline__ float unit_of(float most, float top) {
+  return fminf(fmaxf(ceilf(most - or_zero(top)), kUnitLeast), 127.0f);
 }
 
 // The maximum over the four lane groups that share a row.
@@ -112,7 +110,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x
     if (row >= x.n_rows) continue;
     const uint64_t tok = (uint64_t)x.q0 + row / a.group;
     const uint32_t hq = h * a.group + row % a.group;
-    const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? w.vref / w.l[n] : 0.0f;
+    const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? ldexpf(1.0f / w.l[n], (int)unit_of(w.most[n], w.m[n])) : 0.0f;
     const float lse2 = w.l[n] == 0.0f ? kNegInf : w.m[n] + __builtin_amdgcn_logf(w.l[n]) - lift;
     if (!whole) {
       const uint64_t to = part_place(a, tok, hq) + part;
@@ -355,24 +353,28 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
           if (i > end || i <= begin) sc[n][i >> 2][i & 3] = kNegInf;
       }
     }
-    const float vref = unit_of(w->vref, group_max(vs), &w->vtop);
-    const float vscale = vs / vref, shrink = w->vref / vref;
-    w->vref = vref;
+    const float vlog = __builtin_amdgcn_logf(vs);
     f16x8 p[NQ][2], p_low[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      float top = w->m[n];
+      float mine = kNegInf;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[n][i][j]);
-      top = group_max(top);
-      const float use = top == kNegInf ? 0.0f : top;  // nothing seen yet: every weight is 0
+        for (int j = 0; j < 4; ++j) mine = fmaxf(mine, sc[n][i][j]);
+      const float top = fmaxf(w->m[n], group_max(mine));
+      const float most = fmaxf(w->most[n], group_max(mine + vlog));
+      const float was = unit_of(w->most[n], w->m[n]), unit = unit_of(most, top);
+      const float use = or_zero(top);  // nothing seen yet: every weight is 0
       const float keep = __builtin_amdgcn_exp2f(w->m[n] - use);
+      const float shrink = ldexpf(keep, (int)(was - unit));
+      // (finite, for the weights of 0 where the row does not see the block)
+      const float vscale = fminf(ldexpf(vs, -(int)unit), 3.4028234e38f);
       w->m[n] = top;
+      w->most[n] = most;
       w->l[n] *= keep;
 #pragma unroll
-      for (int i = 0; i < VT; ++i) w->o[n][i] *= keep * shrink;
+      for (int i = 0; i < VT; ++i) w->o[n][i] *= shrink;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -433,7 +435,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
 // joined through LDS, two at a time (a lane's rows are the same in each wave).
 template <int D, int NQ>
 struct Parked {
-  float o[NQ * (D / 4)][64], m[NQ][64], l[NQ][64], vref[64];
+  float o[NQ * (D / 4)][64], m[NQ][64], l[NQ][64], most[NQ][64];
   uint32_t special;
 };
 
@@ -447,23 +449,25 @@ __device__ __forceinline__ void park(const Rows<D, NQ> &w, Parked<D, NQ> *x, int
       for (int j = 0; j < 4; ++j) x->o[n * (D / 4) + 4 * i + j][lane] = w.o[n][i][j];
     x->m[n][lane] = w.m[n];
     x->l[n][lane] = w.l[n];
+    x->most[n][lane] = w.most[n];
   }
-  x->vref[lane] = w.vref;
   if (lane == 0) x->special = w.special;
 }
 
 template <int D, int NQ>
 __device__ __forceinline__ void join(Rows<D, NQ> *w, const Parked<D, NQ> &x, int lane) {
-  const float vx = x.vref[lane], vref = fmaxf(w->vref, vx);
   w->special |= __builtin_amdgcn_readfirstlane(x.special) != 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const float mx = x.m[n][lane], top = fmaxf(w->m[n], mx);
-    const float use = top == kNegInf ? 0.0f : top;
+    const float use = or_zero(top), most = fmaxf(w->most[n], x.most[n][lane]);
+    const float u0 = unit_of(w->most[n], w->m[n]), u1 = unit_of(x.most[n][lane], mx);
+    const float unit = unit_of(most, top);
     const float f0 = __builtin_amdgcn_exp2f(w->m[n] - use), f1 = __builtin_amdgcn_exp2f(mx - use);
     w->m[n] = top;
     w->l[n] = w->l[n] * f0 + x.l[n][lane] * f1;
-    const float g0 = f0 * (w->vref / vref), g1 = f1 * (vx / vref);
+    const float g0 = ldexpf(f0, (int)(u0 - unit)), g1 = ldexpf(f1, (int)(u1 - unit));
+    w->most[n] = most;
     if (w->special) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
@@ -479,7 +483,6 @@ __device__ __forceinline__ void join(Rows<D, NQ> *w, const Parked<D, NQ> &x, int
       for (int j = 0; j < 4; ++j)
         w->o[n][i][j] = w->o[n][i][j] * g0 + x.o[n * (D / 4) + 4 * i + j][lane] * g1;
   }
-  w->vref = vref;
 }
 
 // Workgroups of a CU: two or three waves a SIMD, with a step each under way.
@@ -548,7 +551,7 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // exponential, two fused products and a rounding per score), so little else
 // is done per score: scores are scaled within the exponent's product, which
 // also takes the values' scale (the sum of the weights takes it out again), a
-// row's maximum moves only when it has grown 2^4 fold (weights are at most
+// row's maxima move only when one has grown 2^4 fold (weights are at most
 // 2^15 all the same: the lift is 4 less), and steps that every row sees whole
 // run in a loop without masks.
 //
@@ -671,7 +674,6 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const int w_lo = a.window && p_first + 1 > (int)a.window ? p_first + 1 - (int)a.window : 0;
   Rows<D, NQ> w;
   clear(&w);
-  float vref = w.vref;  // the tile's; w.vref is the one of the wave's last step
   const uint32_t s_part = it.part << (x.cut - 6);
   uint32_t s0 = t.lo >> 6, s1 = none ? 0u : (uint32_t)(((uint64_t)t.hi + 63) >> 6);
   if (s0 < s_part) s0 = s_part;
@@ -779,8 +781,6 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       load(s + 1);
       blocks(s + 2);
     }
-    vref = unit_of(vref, group_max(vs), &w.vtop);
-    const float ratio = fmaxf(vs * __builtin_amdgcn_rcpf(vref), 0x1p-60f);
     __syncthreads();
     const int t0 = (int)(s << 6);
     if (kMasked && (t0 >= w_hi || t0 + 63 < w_lo)) return;  // nothing for this wave
@@ -824,8 +824,9 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       }
     }
     const float f = kMasked ? 1.0f : cs;
-    float top[NQ];
-    bool grows = w.vref != vref;
+    const float vlog = __builtin_amdgcn_logf(vs);
+    float mine[NQ];  // the lane's largest score
+    bool grows = false;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       float y = max3(sc[n][0][0], sc[n][0][1], sc[n][0][2]);
@@ -833,28 +834,33 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
       for (int i = 3; i < 15; i += 2)
         y = max3(y, sc[n][i >> 2][i & 3], sc[n][(i + 1) >> 2][(i + 1) & 3]);
       y = fmaxf(y, sc[n][3][3]) * f;
-      top[n] = group_max(!kMasked && idv < 0 ? kNegInf : y);
-      grows |= top[n] > w.m[n] + kSlack;
+      mine[n] = !kMasked && idv < 0 ? kNegInf : y;
+      grows |= mine[n] > w.m[n] + kSlack || mine[n] + vlog > w.most[n] + kSlack;
     }
     if (__any(grows)) {
-      const float shrink = w.vref / vref;
-      w.vref = vref;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        const float m = fmaxf(w.m[n], top[n]);
-        const float keep = __builtin_amdgcn_exp2f(w.m[n] - (m == kNegInf ? 0.0f : m));
+        const float m = fmaxf(w.m[n], group_max(mine[n]));
+        const float most = fmaxf(w.most[n], group_max(mine[n] + vlog));
+        const float was = unit_of(w.most[n], w.m[n]);
+        const float keep = __builtin_amdgcn_exp2f(w.m[n] - or_zero(m));
+        const float shrink = ldexpf(keep, (int)(was - unit_of(most, m)));
         w.m[n] = m;
+        w.most[n] = most;
         w.l[n] *= keep;
 #pragma unroll
-        for (int i = 0; i < VT; ++i) w.o[n][i] *= keep * shrink;
+        for (int i = 0; i < VT; ++i) w.o[n][i] *= shrink;
       }
     }
-    const float back = __builtin_amdgcn_rcpf(ratio);
-    const float lift = kLiftMany + __builtin_amdgcn_logf(ratio);
     f16x8 p[NQ][2], p_low[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      float add = lift - (w.m[n] == kNegInf ? 0.0f : w.m[n]);
+      // the scale in the row's unit: far below it, it stays in the sum of the
+      // weights alone
+      const int unit = (int)unit_of(w.most[n], w.m[n]);
+      const float ratio = fminf(fmaxf(ldexpf(vs, -unit), 0x1p-60f), 0x1p126f);
+      const float back = __builtin_amdgcn_rcpf(ratio);
+      float add = kLiftMany + __builtin_amdgcn_logf(ratio) - or_zero(w.m[n]);
       if (!kMasked) add = idv < 0 ? kNegInf : add;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {

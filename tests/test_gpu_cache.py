@@ -1063,3 +1063,31 @@ def test_infinite_values_that_every_row_sees(wm, dt, lens, new, heads, group, bt
     assert bool((o[..., 4] == -math.inf).all())
     assert bool(o[..., 5].isnan().all())
     assert bool(torch.isfinite(o[..., [0, 1, 2]]).all()) and bool(torch.isfinite(o[..., 6:]).all())
+
+
+@pytest.mark.parametrize("lens,new,heads,group,bt,dim,dt,fmt,window,first,factor", [
+    # causal: rows of the first block see nothing of the ones after it
+    ([64], [64], 1, 1, 16, 64, BF, E4, 0, 0, 40),
+    ([64], [64], 1, 2, 16, 128, BF, E5, 0, 0, 60),     # 128 rows: prompts
+    ([100, 64], [100, 64], 1, 2, 32, 64, BF, E4, 0, 0, 90),
+    ([80], [80], 2, 2, 16, 192, BF, E4, 0, 0, 40),
+    ([90], [90], 1, 1, 32, 256, BF, E4, 0, 0, 40),
+    ([64], [40], 1, 2, 32, 64, HF, E4, 0, -10, 20),
+    ([50], [30], 1, 1, 32, 256, HF, E4, 0, -10, 20),
+    # behind a window: later rows see nothing of the blocks before it
+    ([64], [64], 1, 1, 16, 64, BF, E4, 9, 60, -50),
+    ([400], [200], 1, 1, 64, 128, BF, E4, 20, 50, -20),
+    ([300], [9], 1, 1, 32, 64, BF, E4, 12, 100, -100),
+])
+def test_scales_of_what_is_not_seen_do_not_count(wm, lens, new, heads, group, bt, dim, dt, fmt,
+                                                 window, first, factor):
+    """Block j's values are scaled by 2^(first + factor j), up to 2^100: a row
+    is as precise as what it sees allows."""
+    def tail(k, v, ks, vs, rows):
+        for row in rows:
+            for j, b in enumerate(row):
+                if b >= 0:
+                    vs[b] *= 2.0 ** max(-100, min(100, first + factor * j))
+
+    check_attend(wm, lens, new, heads, group, bt, dim, dt, fmt, window=window, seed=98, tail=tail,
+                 spread=0.5)
