@@ -107,20 +107,10 @@ __device__ __forceinline__ float weighed(float f, float y) {
 }
 
 // Makes those of the wave's codes x zero that have no finite value; was there
-// one?  (With infinities every step asks, and almost none has one: they are
-// looked for first, 283 and 236 us for prompts in fp16 and bf16 where clearing
-// at once takes 341 and 241.  Without, only masked steps ask, and the branch
-// costs more registers than it saves work: 230 us against 252.)
+// one?
 template <int FMT, int N>
 __device__ __forceinline__ bool take_special(u32x4 (&x)[N]) {
   uint32_t any = 0;
-  if constexpr (Code<FMT>::kInfinities) {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) any |= Code<FMT>::special(x[i][j]);
-    if (!__any((any & 0x80808080u) != 0)) return false;
-  }
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -129,7 +119,7 @@ __device__ __forceinline__ bool take_special(u32x4 (&x)[N]) {
       x[i][j] &= ~((sp >> 7) * 0xFFu);
       any |= sp;
     }
-  return Code<FMT>::kInfinities || __any(any != 0);
+  return __any(any != 0);
 }
 
 // A request as attention sees it.  Its query rows that share a key head are its
