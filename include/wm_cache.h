@@ -134,8 +134,9 @@ wm_status wm_page_tables(const int32_t *old_len, const int32_t *new_len,
  *   code = x / scale, rounded to nearest, ties to even; an infinity becomes
  *   the largest value of its sign, a NaN stays one.
  *   slot_map : n_tokens entries; where the first new token of a block has a
- *              slot below 0 (padding) or beyond the pool (sets WM_C_PAGE),
- *              that block's tokens are not stored
+ *              slot below 0 (padding) or beyond the pool (sets WM_C_PAGE), or
+ *              where the slots of a block's first and last new token do not fit
+ *              consecutive places (sets it too), the block's are not stored
  *   n_tokens : rows that k, v and slot_map have; q_start beyond it sets
  *              WM_C_SLOTS and those tokens are not stored.  Rows behind the
  *              last request's are not read

@@ -376,10 +376,13 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   int64_t end = q0 + (nth + 1) * bt - at;
   end = end < q1 ? end : q1;
   const uint32_t off = nth ? 0u : (uint32_t)at, n_new = (uint32_t)(end - begin);
-  const int64_t slot = nth ? a.slots[begin] : s0;
+  const int64_t slot = nth ? a.slots[begin] : s0, last = a.slots[end - 1];
   if (slot < 0) return;
   const uint64_t page = (uint64_t)slot >> a.bt_log2;
-  if (page >= a.c.n_blocks) {
+  // a later block begins at its first place, and the last token stands where
+  // slots that follow each other put it
+  if (page >= a.c.n_blocks || (nth && (slot & (bt - 1))) ||
+      (uint64_t)last - (uint64_t)slot != n_new - 1u) {
     if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_PAGE);
     return;
   }

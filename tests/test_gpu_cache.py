@@ -1091,3 +1091,27 @@ def test_scales_of_what_is_not_seen_do_not_count(wm, lens, new, heads, group, bt
 
     check_attend(wm, lens, new, heads, group, bt, dim, dt, fmt, window=window, seed=98, tail=tail,
                  spread=0.5)
+
+
+@pytest.mark.parametrize("slots", [
+    [-1] * 3 + list(range(23, 43)),          # padding at the start of a request
+    list(range(16, 32)) + list(range(35, 42)),  # a gap behind a block's last place
+    list(range(16, 31)) + list(range(32, 40)),  # a gap before it
+])
+@pytest.mark.parametrize("requests", [1, 8])  # a workgroup and a wave for a block
+def test_slots_that_do_not_follow_each_other(wm, slots, requests):
+    """Tokens of a later block are not stored at places that they do not have."""
+    bt, n = 16, 23
+    k, v, ks, vs = make_cache(6, 2, bt, 64, E4, 101)
+    before = [t.clone() for t in (k.view(torch.uint8), v.view(torch.uint8), ks, vs)]
+    x = torch.randn(n, 2, 64).to(BF).cuda()
+    starts = dev([0] + [n] * requests)
+    verdict = word()
+    wm.cache_append(x, x, k, v, ks, vs, dev(slots, torch.int64), starts, verdict)
+    assert verdict.item() == 8
+    after = (k.view(torch.uint8), v.view(torch.uint8), ks, vs)
+    # a request's first block is stored if its slots are sound
+    same = [torch.equal(a[2:], b[2:]) for a, b in zip(after, before)]
+    assert all(same) and all(torch.equal(a[0], b[0]) for a, b in zip(after, before))
+    first = all(torch.equal(a[1], b[1]) for a, b in zip(after, before))
+    assert first == (slots[:16] != list(range(16, 32)))
