@@ -178,8 +178,9 @@ wm_status wm_cache_append(const wm_cache *cache, const wm_rows *k,
  *   q_start     : n_requests + 1, ascending.  Starts below 0 or beyond n_tokens
  *                 set WM_C_SLOTS: the rows that are there stand where the
  *                 formula says, the others are not computed
- *   len         : n_requests; a length beyond the table's max_blocks sets
- *                 WM_C_LENGTH and counts as that many tokens
+ *   len         : n_requests; where a request has rows, a length below 0 or
+ *                 beyond the table's max_blocks sets WM_C_LENGTH and counts as
+ *                 0 or as that many tokens
  *   max_len     : host: the longest length, for the split of the work; the
  *                 outputs stay right if a length is larger
  *   verdict     : 1 u32 that bits are ORed into, or NULL

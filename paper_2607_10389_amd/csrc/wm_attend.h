@@ -152,7 +152,7 @@ struct Item {
 
 struct ItemWalk {
   Request *mine;        // LDS: the wave's 64 requests
-  bool tell;            // say so of lengths beyond the table and starts beyond the rows
+  bool tell;            // say so of lengths and starts that are out of range
   uint64_t base = 0;    // items before them
   uint32_t r0 = 0, n = 0, sum = 0, all = 0;  // a lane's items, with those before it, all 64's
 
@@ -644,7 +644,8 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     atomicOr(a.verdict, WM_C_SLOTS);
   if (!find_item(a, requests + 64 * wave, blockIdx.x, &it)) return;
   // (every request with new tokens has an item, whose workgroup speaks for it)
-  if (threadIdx.x == 0 && a.verdict && (int64_t)a.len[it.r] > (int64_t)a.max_blocks << a.bt_log2)
+  if (threadIdx.x == 0 && a.verdict &&
+      (a.len[it.r] < 0 || (int64_t)a.len[it.r] > (int64_t)a.max_blocks << a.bt_log2))
     atomicOr(a.verdict, WM_C_LENGTH);
   const Request &x = it.x;
   const Tile t = tile_of(a, x, it.tile);

@@ -144,10 +144,8 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, uint32_t r, b
   q1 = q1 < (int64_t)a.n_tokens ? q1 : (int64_t)a.n_tokens;
   if (q0 >= q1) return x;
   const int64_t cap = (int64_t)a.max_blocks << a.bt_log2;
-  if (len > cap) {
-    len = cap;
-    if (tell && a.verdict) atomicOr(a.verdict, WM_C_LENGTH);
-  }
+  if (tell && a.verdict && (len < 0 || len > cap)) atomicOr(a.verdict, WM_C_LENGTH);
+  len = len < cap ? len : cap;
   len = len > 0 ? len : 0;
   // (below -2^30 none of up to 2^30 rows sees anything, and differences of
   // positions stay within 32 bits)

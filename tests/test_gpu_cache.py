@@ -1115,3 +1115,23 @@ def test_slots_that_do_not_follow_each_other(wm, slots, requests):
     assert all(same) and all(torch.equal(a[0], b[0]) for a, b in zip(after, before))
     first = all(torch.equal(a[1], b[1]) for a, b in zip(after, before))
     assert first == (slots[:16] != list(range(16, 32)))
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [90, 80, 70]])  # single tokens, prompts
+def test_lengths_below_zero_are_told(wm, new):
+    bt, lens = 16, [100, -5, 80]
+    rows, blocks = layout([100, 0, 80], bt, 103)
+    k, v, ks, vs = make_cache(blocks, 1, bt, 64, E4, 104)
+    starts = [0] + np.cumsum(new).tolist()
+    q = torch.randn(starts[-1], 2, 64).to(BF).cuda()
+    outs = []
+    for ln, want in ((lens, 1), ([100, 0, 80], 0), ([100, 90, -(1 << 31)], 1)):
+        out, lse, verdict = torch.full_like(q, 7.0), torch.zeros(starts[-1], 2, device="cuda"), word()
+        table = dev([rows[0], rows[0], rows[2]])
+        ws = torch.empty(wm.attend_ws_bytes(q, k, dev(ln), 100), dtype=torch.uint8, device="cuda")
+        wm.cache_attend(q, k, v, ks, vs, table, dev(ln), dev(starts), out, ws, max_len=100,
+                        scale=0.2, lse=lse, verdict=verdict)
+        assert verdict.item() == want
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and bool(outs[0].any())
+    assert not outs[2][starts[2]:].any()
