@@ -638,11 +638,12 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
   const uint32_t bt = 1u << a.bt_log2;
   __shared__ Request requests[64 * kWaves];
   Item it;
+  const uint32_t place = blockIdx.y * gridDim.x + blockIdx.x;
   // (starts ascend: those beyond the rows show at either end)
-  if (blockIdx.x == 0 && threadIdx.x == 0 && a.verdict &&
+  if (place == 0 && threadIdx.x == 0 && a.verdict &&
       (a.q_start[0] < 0 || (int64_t)a.q_start[a.n_requests] > (int64_t)a.n_tokens))
     atomicOr(a.verdict, WM_C_SLOTS);
-  if (!find_item(a, requests + 64 * wave, blockIdx.x, &it)) return;
+  if (!find_item(a, requests + 64 * wave, place, &it)) return;
   // (every request with new tokens has an item, whose workgroup speaks for it)
   if (threadIdx.x == 0 && a.verdict &&
       (a.len[it.r] < 0 || (int64_t)a.len[it.r] > (int64_t)a.max_blocks << a.bt_log2))
@@ -965,7 +966,10 @@ template <int DT, int FMT, int D>
 int attend_rows(const AttendArgs &a, hipStream_t st) {
   const uint64_t most = (uint64_t)a.plan.tiles * a.c.n_heads * a.plan.splits;
   if (a.plan.rows > 32) {
-    k_attend_many<DT, FMT, D><<<(uint32_t)most, 64 * many_waves(D), 0, st>>>(a);
+    // (fewer than 2^26: of the 2^30 rows and heads at most, requests have over 32
+    // on average, and where they are many no sequence is cut)
+    const dim3 grid(grid_x((uint32_t)most), grid_y((uint32_t)most));
+    k_attend_many<DT, FMT, D><<<grid, 64 * many_waves(D), 0, st>>>(a);
     return (int)hipGetLastError();
   }
   const uint64_t room = (uint64_t)a.n_cu * resident(D, a.plan.rows / 16);

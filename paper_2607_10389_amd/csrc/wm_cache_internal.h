@@ -56,6 +56,9 @@ struct AttendArgs {
   float scale_log2;  // scale * log2(e)
 };
 int launch_cache_attend(const AttendArgs &a, void *stream);
+// A grid of n workgroups and more on two axes: one axis holds 2^32 threads.
+inline uint32_t grid_x(uint32_t n) { return n < 1u << 22 ? n : 1u << 22; }
+inline uint32_t grid_y(uint32_t n) { return (n - 1u) / (1u << 22) + 1u; }
 // The tiles of one head size (a file each).
 int launch_attend_64(const AttendArgs &a, void *stream);
 int launch_attend_128(const AttendArgs &a, void *stream);

@@ -701,9 +701,7 @@ int launch_cache_attend(const AttendArgs &a, void *stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   const uint64_t waves = (uint64_t)a.n_tokens * a.group * a.c.n_heads;
   const uint32_t units = (uint32_t)((waves + kAttThreads / 64 - 1) / (kAttThreads / 64));
-  // (one axis of a grid holds 2^32 threads)
-  const uint32_t most = 1u << 22;
-  const dim3 grid(units < most ? units : most, (units + most - 1) / most);
+  const dim3 grid(grid_x(units), grid_y(units));
   const bool bf = a.q.dtype == WM_BF16;
   switch (d / 64) {
 #define WM_JOIN(kd)                                                      \

@@ -1135,3 +1135,34 @@ def test_lengths_below_zero_are_told(wm, new):
         outs.append(out)
     assert torch.equal(outs[0], outs[1]) and bool(outs[0].any())
     assert not outs[2][starts[2]:].any()
+
+
+def test_more_workgroups_than_an_axis_of_a_grid_holds(wm):
+    """440 million query vectors in requests of 33 tokens: 17 million tiles.
+    Queries and outputs are one token's, again and again, and every row sees
+    one of a block's equal tokens: one answer for all, an lse for each."""
+    n, each, heads, dim, bt = 840_000, 33, 16, 64, 64
+    g = torch.Generator().manual_seed(105)
+    k = torch.randn(1, heads, 1, dim, generator=g).expand(1, heads, bt, dim).to(E4).contiguous()
+    v = torch.randn(1, heads, dim, 1, generator=g).expand(1, heads, dim, bt).to(E4).contiguous()
+    one = torch.ones(1, heads, device="cuda")
+    q1 = torch.randn(1, heads, dim, generator=g).to(BF)
+    q, out = q1.cuda().expand(n * each, heads, dim), torch.zeros(1, heads, dim, dtype=BF,
+                                                                 device="cuda")
+    lse = torch.full((n * each, heads), 7.0, device="cuda")
+    lens = torch.full((n,), bt, dtype=torch.int32, device="cuda")
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda") * each
+    table, verdict = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), word()
+    say(f"[attend] {n} requests of {each} tokens and {heads} heads")
+    wm.cache_attend(q, k.cuda(), v.cuda(), one, one, table, lens, starts,
+                    out.expand(n * each, heads, dim), max_len=bt, scale=0.125, window=1, lse=lse,
+                    verdict=verdict)
+    torch.cuda.synchronize()
+    assert verdict.item() == 0
+    assert torch.equal(out.float().cpu()[0], v.float()[0, :, :, 0])
+    qk = q1.double()[0] * k.double()[0, :, 0] * 0.125
+    spread, z = qk.abs().sum(-1), qk.sum(-1)
+    zero = torch.zeros(heads, dim, dtype=torch.float64)
+    _, bound = ref.attend_bound(BF, zero, z, zero, spread, 1, dim)
+    assert bool(((lse[0].cpu().double() - z).abs() <= bound).all())
+    assert bool((lse == lse[0]).all())
