@@ -242,6 +242,7 @@ class PoolTable:
 
     def __init__(self, pools):
         self.n = len(pools)
+        self.pools = list(pools)  # the table holds their addresses
         self.t = (Pool * max(self.n, 1))()
         self.device = _device(pools[0]) if self.n else None
         for i, x in enumerate(pools):

@@ -244,6 +244,7 @@ class LeafTable:
 
     def __init__(self, leaves):
         self.n = len(leaves)
+        self.leaves = list(leaves)  # the table holds their addresses
         self.t = (Leaf * max(self.n, 1))()
         for i, x in enumerate(leaves):
             if not x.is_cuda or not x.is_contiguous():

@@ -1166,3 +1166,15 @@ def test_more_workgroups_than_an_axis_of_a_grid_holds(wm):
     _, bound = ref.attend_bound(BF, zero, z, zero, spread, 1, dim)
     assert bool(((lse[0].cpu().double() - z).abs() <= bound).all())
     assert bool((lse == lse[0]).all())
+
+
+def test_tables_of_addresses_keep_their_tensors(wm):
+    import weakref
+    from paper_2607_10389_amd import _wm
+    for make in (wm.PoolTable, _wm.LeafTable):
+        t = torch.zeros(4, 16, dtype=torch.uint8, device="cuda")
+        table, there = make([t]), weakref.ref(t)
+        del t
+        assert there() is not None and there().data_ptr() == table.t[0].ptr
+        del table
+        assert there() is None
