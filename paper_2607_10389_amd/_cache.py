@@ -225,6 +225,8 @@ def cache_attend(q, k_cache, v_cache, k_scale, v_scale, block_table, lens, q_sta
     qr, outr = _rows(q, hq, k_cache.shape[3], dev, "q"), _rows(out, hq, d, dev, "out")
     if out.shape[0] != n or out.dtype is not q.dtype:
         raise ValueError("out has the tokens and type of q")
+    if not (0 <= window < 1 << 31 and 0 <= max_len < 1 << 31):  # (ctypes would cut them)
+        raise ValueError("window and max_len are below 2^31")
     n_req = lens.numel()
     return _run("wm_cache_attend", dev, stream, LIB.wm_cache_attend, c, qr, outr,
                 None if lse is None else _vec(lse, torch.float32, dev, n * hq, "lse"), hq,

@@ -186,3 +186,22 @@ def test_binding_refuses_host_tensors(cache):
         cache.cache_desc(k, k.view(2, 1, 64, 16), torch.zeros(2, 1), torch.zeros(2, 1))
     with pytest.raises(ValueError):
         cache.PoolTable([torch.zeros(4, 4)])
+
+
+def test_binding_refuses_numbers_beyond_32_bits(cache, monkeypatch):
+    import torch
+    calls = []
+    monkeypatch.setattr(cache, "_device", lambda t: t.get_device())
+    monkeypatch.setattr(cache, "_run", lambda *args: calls.append(args))
+    k = torch.zeros(2, 1, 16, 64, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    v, s = k.view(2, 1, 64, 16), torch.zeros(2, 1)
+    q = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    one = torch.ones(1, dtype=torch.int32)
+    args = (q, k, v, s, s, one[None], one, torch.zeros(2, dtype=torch.int32), torch.zeros_like(q))
+    for bad in (dict(window=1 << 32), dict(window=(1 << 32) + 5), dict(window=-1),
+                dict(max_len=1 << 32), dict(max_len=-1)):
+        with pytest.raises(ValueError):
+            cache.cache_attend(*args, **{**dict(max_len=1, scale=1.0), **bad})
+    assert not calls
+    cache.cache_attend(*args, max_len=1, scale=1.0, window=(1 << 31) - 1)
+    assert len(calls) == 1
