@@ -109,7 +109,8 @@ typedef struct wm_rows {
  *                 WM_C_SLOTS; then no table, ring, slot or start changed and
  *                 pool_out is pool_in
  * n_requests 0 is allowed (pool_out is pool_in, q_start[0] is 0).
- * Errors: WM_ERR_INVALID_ARG, WM_ERR_HIP. */
+ * Errors: WM_ERR_INVALID_ARG, WM_ERR_UNSUPPORTED (block_tokens not listed
+ *         above), WM_ERR_HIP. */
 wm_status wm_page_tables(const int32_t *old_len, const int32_t *new_len,
                          uint32_t n_requests, uint32_t block_tokens,
                          int32_t *block_table, uint64_t table_stride,
@@ -131,8 +132,9 @@ wm_status wm_page_tables(const int32_t *old_len, const int32_t *new_len,
  *   any other block keeps its scale s if a <= F s, else the scale becomes
  *   s 2^n with the smallest n that is enough and its older codes are rounded
  *   again to it (a power of two: exact but for values that get subnormal).
- *   code = x / scale, rounded to nearest, ties to even; an infinity becomes
- *   the largest value of its sign, a NaN stays one.
+ *   code = x / scale, rounded to nearest, ties to even (a quotient that is not
+ *   exact, by a scale of the caller's that is no power of two, to 32 bits
+ *   first); an infinity becomes the largest value of its sign, a NaN stays one.
  *   slot_map : n_tokens entries; where the first new token of a block has a
  *              slot below 0 (padding) or beyond the pool (sets WM_C_PAGE), or
  *              where the slots of a block's first and last new token do not fit
@@ -220,7 +222,7 @@ typedef struct wm_pool {
 #define WM_MAX_POOLS 4096
 
 /* Flat size of n_pages pages of each pool; 0 for a NULL table with n_pools
- * above 0 or a sum beyond 2^63.  pools: host array. */
+ * above 0 or a sum beyond 2^62.  pools: host array. */
 uint64_t wm_flat_pages_bytes(const wm_pool *pools, uint32_t n_pools,
                              uint32_t n_pages);
 
