@@ -124,8 +124,11 @@ __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x
                    (uint64_t)hq * a.out.head_stride + 4 * g;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) {
-      const uint32_t u = Qk<DT, FMT>::two(w.o[n][j][0] * inv, w.o[n][j][1] * inv);
-      const uint32_t v = Qk<DT, FMT>::two(w.o[n][j][2] * inv, w.o[n][j][3] * inv);
+      uint32_t u = Qk<DT, FMT>::two(w.o[n][j][0] * inv, w.o[n][j][1] * inv);
+      uint32_t v = Qk<DT, FMT>::two(w.o[n][j][2] * inv, w.o[n][j][3] * inv);
+      // (or the compiler would round product and half apart for one kind of store
+      // and at once for the other, and the bits would depend on the address)
+      asm("" : "+v"(u), "+v"(v));
       if (wide) {
         *(u32x2 *)(op + 16 * j) = u32x2{u, v};
       } else {

@@ -1178,3 +1178,29 @@ def test_tables_of_addresses_keep_their_tensors(wm):
         assert there() is not None and there().data_ptr() == table.t[0].ptr
         del table
         assert there() is None
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("lens,new,group,dim", [([200], [90], 2, 64), ([150, 90], [90, 80], 1, 128),
+                                                ([140], [75], 1, 256), ([900], [9], 3, 64)])
+def test_prompts_at_any_address(wm, dt, lens, new, group, dim):
+    """Queries and outputs that begin at odd elements, with odd strides: the
+    bits of aligned ones, and nothing between the vectors."""
+    say(f"[attend] {dt} lens={lens} new={new} group={group} dim={dim}")
+    bt, heads, total = 32, 2, sum(new)
+    rows, blocks = layout(lens, bt, 115)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, E4, 116)
+    hq, starts = heads * group, [0] + np.cumsum(new).tolist()
+    shape, step = (total, hq, dim), (hq * (dim + 3) + 2, dim + 3, 1)
+    flat = torch.randn(total * step[0] + 1, generator=torch.Generator().manual_seed(117)).to(dt)
+    q = flat.cuda()[1:].as_strided(shape, step)
+    aligned, odd = torch.zeros(shape, dtype=dt, device="cuda"), torch.zeros_like(flat.cuda())
+    args = (k, v, ks, vs, dev(rows), dev(lens), dev(starts))
+    ws = torch.empty(wm.attend_ws_bytes(aligned, k, dev(lens), max(lens)), dtype=torch.uint8,
+                     device="cuda")
+    wm.cache_attend(q.contiguous(), *args, aligned, ws, max_len=max(lens), scale=0.1)
+    view = odd[1:].as_strided(shape, step)
+    wm.cache_attend(q, *args, view, ws, max_len=max(lens), scale=0.1)
+    assert torch.equal(view, aligned) and bool(aligned.any())
+    view.zero_()
+    assert not odd.any()
