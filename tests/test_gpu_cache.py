@@ -1204,3 +1204,110 @@ def test_prompts_at_any_address(wm, dt, lens, new, group, dim):
     assert torch.equal(view, aligned) and bool(aligned.any())
     view.zero_()
     assert not odd.any()
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("new,dim", [([1] * 9, 64), ([3, 1, 8], 128), ([40, 1, 77], 64),
+                                     ([130, 20], 192)])
+def test_rows_at_any_address_are_stored(wm, dt, fmt, new, dim):
+    """Keys and values that begin at odd elements, with odd strides."""
+    say(f"[append] {dt} {fmt} new={new} dim={dim}")
+    bt, heads = 32, 2
+    old = [5 * i for i in range(len(new))]
+    rows, blocks = layout([o + n for o, n in zip(old, new)], bt, 111)
+    k, v, ks, vs = make_cache(blocks, heads, bt, dim, fmt, 112)
+    starts = [0] + np.cumsum(new).tolist()
+    slots = [rows[r][(o + i) // bt] * bt + (o + i) % bt
+             for r, (o, n) in enumerate(zip(old, new)) for i in range(n)]
+    total, g = starts[-1], torch.Generator().manual_seed(113)
+    row, head = heads * (dim + 3) + 4, dim + 3
+    flat = (torch.randn(2 * total * row + 1, generator=g) * 3).to(dt)
+    kn = flat[1:].as_strided((total, heads, dim), (row, head, 1))
+    vn = flat[1 + total * row:].as_strided((total, heads, dim), (row, head, 1))
+    want_k, want_ks = ref.append(kn, k.cpu(), ks.cpu(), slots, starts, False)
+    want_v, want_vs = ref.append(vn, v.cpu(), vs.cpu(), slots, starts, True)
+    there, verdict = flat.cuda(), word()
+    wm.cache_append(there[1:].as_strided((total, heads, dim), (row, head, 1)),
+                    there[1 + total * row:].as_strided((total, heads, dim), (row, head, 1)),
+                    k, v, ks, vs, dev(slots, torch.int64), dev(starts), verdict)
+    assert verdict.item() == 0
+    assert torch.equal(ks.cpu().double(), want_ks) and torch.equal(vs.cpu().double(), want_vs)
+    assert torch.equal(ref.decode(k.cpu()), want_k)
+    assert torch.equal(ref.decode(v.cpu()), want_v)
+
+
+@pytest.mark.parametrize("lens,new,heads,group,more", [
+    # 17 to 32 rows a request at 64 dimensions, over several parts
+    ([1500, 700], [5, 5], 2, 4, {}), ([2100, 30, 600], [1, 1, 1], 1, 32, {}),
+    ([1700], [24], 1, 1, dict(window=900)), ([1300, 1200], [9, 7], 1, 3, dict(max_len=600))])
+def test_tiles_of_32_rows_in_parts(wm, lens, new, heads, group, more):
+    for dt, fmt in ((BF, E4), (HF, E5)):
+        check_attend(wm, lens, new, heads, group, 16, 64, dt, fmt, seed=120, **more)
+
+
+def test_a_prompt_in_a_mostly_empty_cache():
+    """One session among 64 places for them, prompt and token: as good as in a
+    cache of its own."""
+    from paper_2607_10389_amd import PagedCache
+    heads, dim, bt, n = 2, 64, 16, 150
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x = [torch.randn(m, 8 * heads, dim, generator=g, device="cuda").to(BF) for m in (n, 1)]
+    for places in (64, 1):
+        c = PagedCache(layers=1, blocks=20, heads=heads, dim=dim, block_tokens=bt,
+                       max_requests=places)
+        for i, y in enumerate(x):
+            assert c.step({places // 2: n + i}) == y.shape[0]
+            c.append(0, y[:, 6 * heads:7 * heads], y[:, 7 * heads:])
+            lse = torch.zeros(y.shape[0], 6 * heads, device="cuda")
+            out = c.attend(0, y[:, :6 * heads], 0.125, lse=lse)
+            k, v, ks, vs = c.layer(0)
+            want, z, weight, sp = ref.attend(
+                y[:, :6 * heads].cpu(), values(k, ks, False), values(v, vs, True),
+                c.block_table[places // 2:places // 2 + 1].tolist(), [n + i], [0, y.shape[0]], bt,
+                0.125)
+            bo, bl = ref.attend_bound(BF, want, z, weight, sp, n + i, dim)
+            assert bool(((out.cpu().double() - want).abs() <= bo).all())
+            assert bool(((lse.cpu().double() - z).abs() <= bl).all())
+
+
+def test_captured_prompts_and_pages_replay(wm):
+    """A prompt in parts, and a session's blocks out of one pool and into
+    another, captured and replayed with new inputs, each time as the eager
+    calls."""
+    bt, lens, new, dim = 32, [1900, 400], [40, 30], 128
+    rows, blocks = layout(lens, bt, 121)
+    k, v, ks, vs = make_cache(blocks, 1, bt, dim, E4, 122)
+    args = (k, v, ks, vs, dev(rows), dev(lens), dev([0, 40, 70]))
+    q = torch.zeros(70, 2, dim, dtype=BF, device="cuda")
+    out, lse = torch.zeros_like(q), torch.zeros(70, 2, device="cuda")
+    ws = torch.empty(wm.attend_ws_bytes(q, k, args[5], 1900), dtype=torch.uint8, device="cuda")
+    assert ws.numel()
+    pool, other = random_bytes(20 * 300, 1).view(20, 300), random_bytes(20 * 300, 2).view(20, 300)
+    pages, to, verdict = dev([7, 7, 3, 19]), dev([0, 4, 8, 2]), word()
+    flat = torch.zeros(wm.flat_pages_bytes([pool], 4), dtype=torch.uint8, device="cuda")
+    tables = wm.PoolTable([pool]), wm.PoolTable([other])
+
+    def calls(o, z):
+        wm.cache_attend(q, *args, o, ws, max_len=1900, scale=0.1, lse=z)
+        wm.flatten_pages(tables[0], pages, flat, verdict)
+        wm.rehydrate_pages(flat, tables[1], to, verdict)
+
+    calls(out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(out, lse)
+    g = torch.Generator(device="cuda").manual_seed(123)
+    for i in range(5):
+        q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+        pages.copy_(torch.randint(0, 20, (4,), generator=g, device="cuda"))
+        pool.copy_(random_bytes(20 * 300, 10 + i).view(20, 300))
+        expect = other.clone()
+        expect[to.long()] = pool[pages.long()]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(other, expect) and verdict.item() == 0, i
+        want, z = torch.zeros_like(out), torch.zeros_like(lse)
+        wm.cache_attend(q, *args, want, ws, max_len=1900, scale=0.1, lse=z)
+        assert torch.equal(out, want) and torch.equal(lse, z) and bool(out.any()), i
