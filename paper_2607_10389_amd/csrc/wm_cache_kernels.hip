@@ -379,10 +379,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
   const int64_t slot = nth ? a.slots[begin] : s0, last = a.slots[end - 1];
   if (slot < 0) return;
   const uint64_t page = (uint64_t)slot >> a.bt_log2;
-  // a later block begins at its first place, and the last token stands where
-  // slots that follow each other put it
-  if (page >= a.c.n_blocks || (nth && (slot & (bt - 1))) ||
-      (uint64_t)last - (uint64_t)slot != n_new - 1u) {
+  // (a later block begins at its first place)
+  if (page >= a.c.n_blocks || (nth && (slot & (bt - 1)))) {
     if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_PAGE);
     return;
   }
@@ -415,6 +413,12 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = amax;
     __syncthreads();  // (and every thread has read the scale)
     for (int i = 0; i < kAppThreads / 64; ++i) amax = fmaxf(amax, part[i]);
+  }
+  // The last token stands where slots that follow each other put it?  (Asked
+  // here, its slot has come while the rows did.)
+  if ((uint64_t)last - (uint64_t)slot != n_new - 1u) {
+    if (tid == 0 && a.verdict) atomicOr(a.verdict, WM_C_PAGE);
+    return;
   }
   const float now = raise_scale<FMT>(was, amax, fresh);
   if (tid == 0 && now != was) *sp = now;
