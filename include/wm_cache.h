@@ -165,6 +165,8 @@ wm_status wm_cache_append(const wm_cache *cache, const wm_rows *k,
  * included; a value that is not finite reaches every row that sees it, however
  * small its weight.  Scores, softmax and sums are in 32 bits.  One query row per
  * request is the form for single tokens; many are a prompt or a chunk of it.
+ * (The kernel goes by the mean of rows per request: a prompt and many single
+ * tokens are faster in two calls than in one.)
  * With up to 32 query heads to a key head, a single token gets the same bits
  * in any call of single tokens whose max_len is not below its length.
  * Weights, times the scales of their values, are rounded to 11 bits for bf16

@@ -270,7 +270,8 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
   // A step's keys are loaded while the step before is between its two
   // products, its values while its own scores are computed: each load has a
   // product and a softmax to arrive in, with one step's registers.  (256
-  // dimensions have none left for that.)
+  // dimensions have none left for that; 192 spill about 60 for it, and 256
+  // about 24 without.)
   constexpr bool kAhead = D < 256;
   u32x4 kr[4][KC], vr[VT];
   float ks = 0.0f, vs = 0.0f;
@@ -336,7 +337,9 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
         }
       }
     if (kAhead && more) load_keys(block_of(ek, t0 + 256 + 16 * ka), t0 + 256);
-    // masks: only where some row does not see some of the 64 tokens
+    // masks: only where some row of the tile does not see some of the 64 tokens
+    // (places behind the request's last row see none, so a tile that is not
+    // full masks every step)
     const float cs = ks * a.scale_log2;
     const int first = (int)(t0 + 16 * g);  // the lane's first token
     bool partial = idv < 0;
@@ -495,10 +498,10 @@ constexpr int resident(int d, int nq) {
 
 // Few rows: the grid is as large as the GPU holds, its workgroups take the
 // items in turn.  HBM bounds it: 32 sessions of 24,576 to 32,768 tokens, 8 key
-// heads of 128, read 1.9 GB in 376 us (5.0 TB/s); eight of 7,296 tokens and 16
-// heads 239 MB in 52 us (4.6); 64 of 1 to 8,192 tokens 118 MB in 32 us (3.7),
+// heads of 128, read 1.9 GB in 374 us (5.1 TB/s); eight of 7,296 tokens and 16
+// heads 239 MB in 52 us (4.6); 64 of 1 to 8,192 tokens 118 MB in 31 us (3.8),
 // where parts of 512 tokens share 512 workgroups unevenly.  One session of 512
-// tokens takes 9.2 us: the chain lengths, table, keys, softmax, join.
+// tokens takes 9.1 us: the chain lengths, table, keys, softmax, join.
 template <int DT, int FMT, int D, int NQ>
 __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendArgs a) {
   __shared__ Parked<D, NQ> parked[2];
@@ -548,7 +551,8 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // exponentials (three or four blocks read LDS less often, but were slower:
 // 288 and 524 us where two took 256).  192 dimensions and more: eight waves
 // with a block each, so that the sums still fit into 256 registers; the tile
-// is 128 rows either way.
+// is 128 rows either way.  (Spilled: 46 and 51 registers at 128 dimensions, 86
+// over e5m2; up to 9 at 192, 32 to 44 at 256, none at 64.)
 //
 // What bounds it is the vector ALU beside the matrix cores (half a maximum, an
 // exponential, two fused products and a rounding per score), so little else
@@ -559,8 +563,8 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // run in a loop without masks.
 //
 // Measured: 2,048 new tokens over 16,384 for four sessions, 32 query heads of
-// 128, at 890 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500 to 2,048
-// over 1 to 4,096 in 227 us, 640 TFLOP/s.  A step takes 1.15 us a workgroup,
+// 128, in 2,492 us, 937 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500
+// to 2,048 over 1 to 4,096 in 226 us, 640 TFLOP/s.  A step takes 1.15 us a workgroup,
 // of which the matrix cores are busy 0.43; a tile's start and end take about
 // 10 us, a third of it for 64 KiB of queries and results.
 constexpr float kSlack = 4.0f, kLiftMany = 11.0f;

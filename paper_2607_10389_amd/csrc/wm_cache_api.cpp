@@ -130,6 +130,9 @@ AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   if (!n_requests || !n_tokens || !n_heads || n_q_heads < n_heads) return p;
   const uint64_t rows = (uint64_t)n_tokens * (n_q_heads / n_heads), each = rows / n_requests;
   const uint64_t len = std::max<uint64_t>(1, max_len);
+  // The mean of the rows per request decides, requests without rows counted:
+  // lengths of rows are known on the device alone.  (So a prompt beside many
+  // single tokens, or among many empty places, takes the others' kernel.)
   // Tiles of 128 rows read the cache once for all of a request's rows and keep
   // the matrix cores busier; small tiles spread it over the CUs in parts.  With
   // 64 rows per request and head 64 requests of 4112 tokens, 8 heads of 128,
@@ -140,8 +143,8 @@ AttendPlan attend_plan(uint32_t n_requests, uint32_t n_tokens, uint32_t n_heads,
   if (each > 64 || (each > 32 && busy > 128))
     p.rows = 128;
   else if (each > 16 && head_dim <= 64)
-    p.rows = 32;  // (larger heads: two tiles of 16 read twice, but 617 -> 425 us at 256
-                  // dimensions, 220 -> 202 at 128; at 64 it is 103 -> 113)
+    p.rows = 32;  // (larger heads: two tiles of 16 read twice, but 617 -> 428 us at 256
+                  // dimensions, 220 -> 209 at 128; at 64 it is 103 -> 113)
   p.tiles = (uint32_t)(rows / p.rows + n_requests);
   if (p.rows > 32) {
     // a sequence is cut only where its tiles leave more than half of 256 CUs idle

@@ -20,8 +20,8 @@ namespace {
 // a table entry is read only where it was in use before.  256 or 2048 requests
 // need one scan, more a first pass for the totals.
 // What bounds it is the chain lengths - scan - search - ring - store: 3.8 us
-// for a step of 64 requests; 10.8 us for 1500 requests with 1.08 M new tokens
-// (8.7 MB of slots, 0.8 TB/s), of which an empty kernel takes about 3.  Shared
+// for a step of 64 requests; 10 to 11 us for 1500 requests with 1.08 M new
+// tokens (8.7 MB of slots, 0.8 TB/s), of which an empty kernel takes about 3.  Shared
 // arrays are written in 16-byte pieces and sums kept in 32 bits (saturating):
 // both together took 4 of 15 us off that.
 struct Step {
@@ -342,8 +342,8 @@ __device__ __forceinline__ void load_eight(const void *p, uint64_t at, float *x)
 // stores eight words of four tokens, its neighbours the next four tokens, so
 // that 16 threads read 64 bytes of a row and write 64 bytes of one.
 // What bounds it: HBM for prompts (24 of them into 16 heads of 128: 227 MB in
-// 58 us, 3.9 TB/s, where a plain copy reaches 4.8); for single tokens a chain
-// of four loads (starts, slot, row and scale, codes): 64 of them in 7.0 us.
+// 59 us, 3.9 TB/s, where a plain copy reaches 4.8); for single tokens a chain
+// of four loads (starts, slot, row and scale, codes): 64 of them in 7.2 us.
 // (Pieces of 16 tokens held in registers from the first pass to the second
 // took 83 us and 160 us: too few threads with a load under way.)
 template <int DT, int FMT, int NT, bool WIDE>
@@ -530,8 +530,8 @@ __global__ __launch_bounds__(kAppThreads) void k_cache_append(AppendArgs a) {
 
 // A wave takes one query row: its parts' sums in one load (a lane each), then
 // the weighted sum of the parts in their order.  Eight parts are loaded at
-// once, or the chain of loads would bound it: 5.1 us for 128 rows of 15 parts,
-// 10.1 us for 2048 rows of 16 to 31.
+// once, or the chain of loads would bound it: 4.7 us for 128 rows of 15 parts,
+// 9.9 us for 2048 rows of 16 to 31.
 template <int DT, int KD>
 __global__ __launch_bounds__(kAttThreads) void k_attend_join(AttendArgs a) {
   const uint32_t hq_all = a.group * a.c.n_heads;

@@ -7,8 +7,13 @@ requests room for their new tokens (or takes it back), ``append`` and
 ``attend`` are one layer's store and attention for those tokens, and
 ``suspend`` / ``resume`` are a session's way out and in: a flat state of every
 layer's blocks, which a ``Mover`` ships like any other, into whichever blocks
-the destination has free.  The session's answers after a move are the same
-bits as before it: they do not depend on where its blocks lie.
+the destination has free.  A token's answers after a move are the same bits as
+before it, in any call of single tokens with up to 32 query heads per key head:
+they do not depend on where its blocks lie or who else is asked.  (A call that
+holds prompts too may take another kernel, whose results differ by roundings.
+The kernel goes by the mean of new tokens per place for a request, empty ones
+counted: long prompts are answered fastest in a cache without many of those,
+or in a call of their own.)
 
 ``append`` and ``attend`` may be captured into a graph and replayed after any
 later ``step`` of no more tokens: tables, lengths, slot map and row starts keep

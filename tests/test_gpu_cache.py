@@ -1311,3 +1311,23 @@ def test_captured_prompts_and_pages_replay(wm):
         want, z = torch.zeros_like(out), torch.zeros_like(lse)
         wm.cache_attend(q, *args, want, ws, max_len=1900, scale=0.1, lse=z)
         assert torch.equal(out, want) and torch.equal(lse, z) and bool(out.any()), i
+
+
+def test_a_token_is_answered_the_same_among_empty_places(wm):
+    """32 query heads per key head at 64 dimensions: tiles of 32 rows, and of 16
+    where most requests have no token."""
+    bt, group, dim, n = 16, 32, 64, 1400
+    rows, blocks = layout([n], bt, 131)
+    for dt, fmt in ((BF, E4), (HF, E4), (BF, E5)):
+        k, v, ks, vs = make_cache(blocks, 1, bt, dim, fmt, 132)
+        q = torch.randn(1, group, dim, generator=torch.Generator().manual_seed(133)).to(dt).cuda()
+        outs = []
+        for places in (1, 2, 5):
+            lens, starts = dev([n] * places), dev([0] + [1] * places)
+            out, lse = torch.zeros_like(q), torch.zeros(1, group, device="cuda")
+            ws = torch.empty(wm.attend_ws_bytes(q, k, lens, n), dtype=torch.uint8, device="cuda")
+            wm.cache_attend(q, k, v, ks, vs, dev(rows * places), lens, starts, out, ws, max_len=n,
+                            scale=0.1 if fmt == E4 else 1e-3, lse=lse)
+            outs.append((out, lse))
+        for o, z in outs[1:]:
+            assert torch.equal(o, outs[0][0]) and torch.equal(z, outs[0][1]) and bool(o.any())
