@@ -19,7 +19,7 @@ template <int D, int NQ>
 struct Rows {
   f32x4 o[NQ][D / 16];
   float m[NQ], l[NQ];  // maximum of the scores (base 2) and sum of the weights
-  float most[NQ];      // maximum of weight times scale (base 2)
+  float most[NQ];      // maximum of weight times scale (base 2, from m on)
   bool special;        // (the whole wave's) values that are not finite were added
 };
 
@@ -40,11 +40,12 @@ __device__ __forceinline__ float or_zero(float x) { return x == kNegInf ? 0.0f :
 
 // The unit of a row's value sums, 2^(unit - kLift) with a whole number, where
 // `most` is the largest weight times scale of what the row has seen (base 2, as
-// scores are) and `top` its largest score.  So the parts that make up the sum
-// are rounded to half precision with all their bits, whether the weight is
-// large or the scale, and what the row does not see has no say in it.
-__device__ __forceinline__ float unit_of(float most, float top) {
-  return fminf(fmaxf(ceilf(most - or_zero(top)), kUnitLeast), 127.0f);
+// scores are, and taken from the largest score, or scores of millions would
+// leave it no bits).  So the parts that make up the sum are rounded to half
+// precision with all their bits, whether the weight is large or the scale, and
+// what the row does not see has no say in it.
+__device__ __forceinline__ float unit_of(float most) {
+  return fminf(fmaxf(ceilf(most), kUnitLeast), 127.0f);
 }
 
 // The maximum over the four lane groups that share a row.
@@ -110,7 +111,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs &a, const Request &x
     if (row >= x.n_rows) continue;
     const uint64_t tok = (uint64_t)x.q0 + row / a.group;
     const uint32_t hq = h * a.group + row % a.group;
-    const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? ldexpf(1.0f / w.l[n], (int)unit_of(w.most[n], w.m[n])) : 0.0f;
+    const float inv = w.l[n] > 0.0f || w.l[n] != w.l[n] ? ldexpf(1.0f / w.l[n], (int)unit_of(w.most[n])) : 0.0f;
     const float lse2 = w.l[n] == 0.0f ? kNegInf : w.m[n] + __builtin_amdgcn_logf(w.l[n]) - lift;
     if (!whole) {
       const uint64_t to = part_place(a, tok, hq) + part;
@@ -369,9 +370,9 @@ __device__ __forceinline__ void attend_steps(const AttendArgs &a, uint32_t r, co
 #pragma unroll
         for (int j = 0; j < 4; ++j) mine = fmaxf(mine, sc[n][i][j]);
       const float top = fmaxf(w->m[n], group_max(mine));
-      const float most = fmaxf(w->most[n], group_max(mine + vlog));
-      const float was = unit_of(w->most[n], w->m[n]), unit = unit_of(most, top);
       const float use = or_zero(top);  // nothing seen yet: every weight is 0
+      const float most = fmaxf(w->most[n] + (w->m[n] - use), group_max(mine - use + vlog));
+      const float was = unit_of(w->most[n]), unit = unit_of(most);
       const float keep = __builtin_amdgcn_exp2f(w->m[n] - use);
       const float shrink = ldexpf(keep, (int)(was - unit));
       // (finite, for the weights of 0 where the row does not see the block)
@@ -466,9 +467,9 @@ __device__ __forceinline__ void join(Rows<D, NQ> *w, const Parked<D, NQ> &x, int
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const float mx = x.m[n][lane], top = fmaxf(w->m[n], mx);
-    const float use = or_zero(top), most = fmaxf(w->most[n], x.most[n][lane]);
-    const float u0 = unit_of(w->most[n], w->m[n]), u1 = unit_of(x.most[n][lane], mx);
-    const float unit = unit_of(most, top);
+    const float use = or_zero(top), r0 = w->most[n], r1 = x.most[n][lane];
+    const float most = fmaxf(r0 + (w->m[n] - use), r1 + (mx - use));
+    const float u0 = unit_of(r0), u1 = unit_of(r1), unit = unit_of(most);
     const float f0 = __builtin_amdgcn_exp2f(w->m[n] - use), f1 = __builtin_amdgcn_exp2f(mx - use);
     w->m[n] = top;
     w->l[n] = w->l[n] * f0 + x.l[n][lane] * f1;
@@ -752,6 +753,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
     vs1 = a.c.v_scale[(uint64_t)(idv1 < 0 ? 0 : idv1) * a.c.v_scale_stride + h];
   };
   uint32_t sp_first = ~0u, sp_last = 0;  // steps with values that the wave took out
+  bool far = false;  // maxima of the wave's rows beyond 2^20
   auto step = [&](uint32_t s, auto mask_tag) {
     constexpr bool kMasked = decltype(mask_tag)::value;
     const int b = s & 1;
@@ -839,36 +841,56 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
         y = max3(y, sc[n][i >> 2][i & 3], sc[n][(i + 1) >> 2][(i + 1) & 3]);
       y = fmaxf(y, sc[n][3][3]) * f;
       mine[n] = !kMasked && idv < 0 ? kNegInf : y;
-      grows |= mine[n] > w.m[n] + kSlack || mine[n] + vlog > w.most[n] + kSlack;
+      const float d = mine[n] - w.m[n];
+      grows |= d > kSlack || d + vlog > w.most[n] + kSlack;
     }
     if (__any(grows)) {
+      bool high = false;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         const float m = fmaxf(w.m[n], group_max(mine[n]));
-        const float most = fmaxf(w.most[n], group_max(mine[n] + vlog));
-        const float was = unit_of(w.most[n], w.m[n]);
-        const float keep = __builtin_amdgcn_exp2f(w.m[n] - or_zero(m));
-        const float shrink = ldexpf(keep, (int)(was - unit_of(most, m)));
+        const float use = or_zero(m);
+        const float most = fmaxf(w.most[n] + (w.m[n] - use), group_max(mine[n] - use + vlog));
+        const float keep = __builtin_amdgcn_exp2f(w.m[n] - use);
+        const float shrink = ldexpf(keep, (int)(unit_of(w.most[n]) - unit_of(most)));
         w.m[n] = m;
         w.most[n] = most;
         w.l[n] *= keep;
+        high |= fabsf(use) > 0x1p20f;
 #pragma unroll
         for (int i = 0; i < VT; ++i) w.o[n][i] *= shrink;
       }
+      far = __any(high);
     }
+    // Scores of a million and more leave the sum of exponents that follows no
+    // bits: their maximum is taken off first, as they were rounded for it.
+    if (far) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float y = sc[n][i >> 2][i & 3] * f;
+          sc[n][i >> 2][i & 3] = y - or_zero(w.m[n]);
+        }
+    }
+    const float fs = far ? 1.0f : f;
     f16x8 p[NQ][2], p_low[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       // the scale in the row's unit: far below it, it stays in the sum of the
-      // weights alone
-      const int unit = (int)unit_of(w.most[n], w.m[n]);
+      // weights alone.  (The empty asm keeps the compiler from carrying the unit
+      // through the branch above, which took 100 registers.)
+      float most = w.most[n];
+      asm("" : "+v"(most));
+      const int unit = (int)unit_of(most);
       const float ratio = fminf(fmaxf(ldexpf(vs, -unit), 0x1p-60f), 0x1p126f);
       const float back = __builtin_amdgcn_rcpf(ratio);
-      float add = kLiftMany + __builtin_amdgcn_logf(ratio) - or_zero(w.m[n]);
+      float add = kLiftMany + __builtin_amdgcn_logf(ratio) - or_zero(far ? 0.0f : w.m[n]);
       if (!kMasked) add = idv < 0 ? kNegInf : add;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i >> 2][i & 3], f, add));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][i >> 2][i & 3], fs, add));
         w.l[n] = __builtin_fmaf(y, back, w.l[n]);
         const _Float16 hi = (_Float16)y;
         p[n][i >> 3][i & 7] = hi;
@@ -939,6 +961,7 @@ __global__ __launch_bounds__(64 * many_waves(D), 2) void k_attend_many(AttendArg
         for (int j = 0; j < 4; ++j) none = __builtin_fmaf(w.o[n][i][j], 0.0f, none);
     if (!__syncthreads_or(!(none == 0.0f))) break;
     clear(&w);
+    far = false;
     sp_first = ~0u;
     sp_last = 0;
     s_b = s_a = s0;

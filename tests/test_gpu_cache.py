@@ -1331,3 +1331,58 @@ def test_a_token_is_answered_the_same_among_empty_places(wm):
             outs.append((out, lse))
         for o, z in outs[1:]:
             assert torch.equal(o, outs[0][0]) and torch.equal(z, outs[0][1]) and bool(o.any())
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("order", ["up", "down", "mixed"])
+@pytest.mark.parametrize("new,group,bt,dim,window", [
+    (1, 16, 16, 64, 0), (1, 4, 64, 256, 50), (126, 2, 16, 64, 0), (100, 2, 64, 128, 0),
+    (126, 1, 32, 192, 20), (120, 2, 128, 256, 0)])
+@pytest.mark.parametrize("high", [2.0 ** 20, 2.0 ** 27, 2.0 ** 40])
+def test_scores_beyond_the_bits_of_32(wm, dt, order, new, group, bt, dim, window, high):
+    """Scores up to `high`: where a row's largest is 64 above the next (the others
+    then weigh less than 126 e^-64 together), its answer is that token's value,
+    whatever the scales; the rows of small scores by the bound of all tests."""
+    n, scale = 126, high / 2.0 ** 14
+    rows, blocks = layout([n], bt, 141)
+    k, v, ks, vs = make_cache(blocks, 1, bt, dim, E4, 142, spread=False)
+    codes = torch.arange(1, 127)
+    if order != "up":
+        codes = codes.flip(0) if order == "down" else codes[torch.randperm(
+            126, generator=torch.Generator().manual_seed(143))]
+    place = [(rows[0][j // bt], j % bt) for j in range(n)]
+    kb = torch.zeros(blocks, 1, bt, dim, dtype=torch.uint8)
+    for (b, t), c in zip(place, codes.tolist()):
+        kb[b, 0, t, 0] = c
+    k.view(torch.uint8).copy_(kb)
+    ks.fill_(1.0)
+    q = torch.zeros(new, group, dim, dtype=dt)
+    q[..., 0] = 32.0
+    out = torch.zeros(new, group, dim, dtype=dt, device="cuda")
+    lse = torch.zeros(new, group, device="cuda")
+    wm.cache_attend(q.cuda(), k, v, ks, vs, dev(rows), dev([n]), dev([0, new]), out, max_len=n,
+                    scale=scale, window=window, lse=lse)
+    vals = values(v, vs, True)
+    score = torch.tensor([float(ref.decode(k.cpu())[b, 0, t, 0]) for b, t in place]) * 32 * scale
+    o, z = out.cpu().double(), lse.cpu().double()
+    for i in range(new):
+        p = n - new + i
+        lo = max(0, p - window + 1) if window else 0
+        two = torch.cat([score[lo:p + 1], torch.tensor([-math.inf])]).topk(2).values
+        j = lo + int(score[lo:p + 1].argmax())
+        if two[0] - two[1] >= 64:
+            want = vals[place[j][0], 0, place[j][1]].to(dt).double()
+            assert torch.equal(o[i], want.expand(group, dim)), (i, j)
+            # lse: the sum of the weights is near 2^11 or 2^15, its logarithm and
+            # the two sums after it each off by up to 2^-21 of 1, the score by
+            # 2^-23 of itself: within the bound of all tests
+            zero = torch.zeros(1, 1, dtype=torch.float64)
+            _, bl = ref.attend_bound(dt, zero[..., None], score[j].double() + zero,
+                                     zero[..., None], score[j].double() + zero, n, dim)
+            assert bool(((z[i] - score[j].double()).abs() <= bl).all()), (i, j)
+            continue
+        got = ref.attend(q[i:i + 1], values(k, ks, False), vals, rows, [p + 1], [0, 1], bt, scale,
+                         window)
+        bo, bl = ref.attend_bound(dt, *got, n, dim)
+        assert bool(((o[i] - got[0][0]).abs() <= bo[0]).all()), (i, j)
+        assert bool(((z[i] - got[1][0]).abs() <= bl[0]).all()), (i, j)
