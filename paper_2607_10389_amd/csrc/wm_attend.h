@@ -500,7 +500,7 @@ constexpr int resident(int d, int nq) {
 // Few rows: the grid is as large as the GPU holds, its workgroups take the
 // items in turn.  HBM bounds it: 32 sessions of 24,576 to 32,768 tokens, 8 key
 // heads of 128, read 1.9 GB in 374 us (5.1 TB/s); eight of 7,296 tokens and 16
-// heads 239 MB in 52 us (4.6); 64 of 1 to 8,192 tokens 118 MB in 31 us (3.8),
+// heads 239 MB in 52 us (4.6); 64 of 1 to 8,192 tokens 118 MB in 32 us (3.7),
 // where parts of 512 tokens share 512 workgroups unevenly.  One session of 512
 // tokens takes 9.1 us: the chain lengths, table, keys, softmax, join.
 template <int DT, int FMT, int D, int NQ>
@@ -552,8 +552,8 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // exponentials (three or four blocks read LDS less often, but were slower:
 // 288 and 524 us where two took 256).  192 dimensions and more: eight waves
 // with a block each, so that the sums still fit into 256 registers; the tile
-// is 128 rows either way.  (Spilled: 46 and 51 registers at 128 dimensions, 86
-// over e5m2; up to 9 at 192, 32 to 44 at 256, none at 64.)
+// is 128 rows either way.  (Spilled: 46 and 55 registers at 128 dimensions, 81
+// and 105 over e5m2; up to 9 at 192, 32 to 45 at 256, none at 64.)
 //
 // What bounds it is the vector ALU beside the matrix cores (half a maximum, an
 // exponential, two fused products and a rounding per score), so little else
@@ -564,8 +564,8 @@ __global__ __launch_bounds__(kAttThreads, resident(D, NQ)) void k_attend(AttendA
 // run in a loop without masks.
 //
 // Measured: 2,048 new tokens over 16,384 for four sessions, 32 query heads of
-// 128, in 2,492 us, 937 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500
-// to 2,048 over 1 to 4,096 in 226 us, 640 TFLOP/s.  A step takes 1.15 us a workgroup,
+// 128, in 2,486 us, 940 TFLOP/s (a bf16 library product of 8192^3: 1300); 1,500
+// to 2,048 over 1 to 4,096 in 228 us, 640 TFLOP/s.  A step takes 1.15 us a workgroup,
 // of which the matrix cores are busy 0.43; a tile's start and end take about
 // 10 us, a third of it for 64 KiB of queries and results.
 constexpr float kSlack = 4.0f, kLiftMany = 11.0f;
